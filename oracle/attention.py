@@ -480,3 +480,60 @@ def cpvm_galois(n: int, c_count: int, d2: int):
     gs = [galois_rot(n, sh) for sh in cpvm_shifts(c_count)]
     gs += [galois_rot(n, sh) for sh in block_shifts(n, d2)] + [galois_swap(n)]
     return sorted(set(gs))
+
+
+# ---------------------------------------------------------------------------
+# Many requests: projections with adapters, position biases, appends at each request's own length
+# ---------------------------------------------------------------------------
+def low_rank_matrix(w, a, b):
+    """W + A B over the integers; w, or a and b, may be None."""
+    m = 0 if a is None else np.asarray(a, dtype=object) @ np.asarray(b, dtype=object)
+    return np.asarray(m if w is None else np.asarray(w, dtype=object) + m, dtype=object)
+
+
+def cpvm_with_adapter(orc, x_ct, diag_polys, adapter_polys, gks, d2: int, w: int = 0):
+    """cpvm_hoisted with the products of an adapter's diagonals (None: no adapter) added before the sum over
+    residue classes."""
+    n, C = orc.n, len(diag_polys)
+    copies = [x_ct] + orc.rotate_many(x_ct, [galois_rot(n, c) for c in range(1, C)], gks)
+    terms = [orc.mul_plain(copies[c], diag_polys[c]) for c in range(C)]
+    if adapter_polys is not None:
+        terms += [orc.mul_plain(copies[c], adapter_polys[c]) for c in range(C)]
+    y = terms[0]
+    for term in terms[1:]:
+        y = orc.add(y, term)
+    gs = block_generators(n, d2)
+    if w:
+        return fold_by_rounds(orc, y, gs, gks, w)
+    for g in gs:
+        y = orc.add(y, orc.rotate(y, g, gks[g]))
+    return y
+
+
+def bias_of(dist: int, table, edges, h: int) -> int:
+    """The table's entry of the last bucket that begins at or below the distance; 0 for none, and for later tokens."""
+    n = -1
+    for i, e in enumerate(edges):
+        if e <= dist:
+            n = i
+    return int(table[n][h]) if dist >= 0 and n >= 0 else 0
+
+
+def score_bias_values(n: int, d: int, c: int, pos: int, table, edges, h: int) -> np.ndarray:
+    """Slot values added to the scores of cache ciphertext c for a token at index pos."""
+    v = np.zeros(n, dtype=np.int64)
+    for b in range(n // d):
+        v[b * d] = bias_of(pos - (c * (n // d) + b), table, edges, h) if pos >= 0 else 0
+    return v
+
+
+def prompt_bias_values(n: int, d: int, unit: int, table, edges, h: int) -> np.ndarray:
+    """Slot values added to diagonal `unit` of prefill_qk."""
+    m = n // d
+    half = m // 2
+    sigma, r = divmod(unit, half)
+    v = np.zeros(n, dtype=np.int64)
+    for i in range(m):
+        row, at = divmod(i, half)
+        v[i * d] = bias_of(i - ((row ^ sigma) * half + (at + r) % half), table, edges, h)
+    return v

@@ -1,4 +1,4 @@
-"""ctypes binding of include/cryptogen.h -- argument marshalling only.
+"""ctypes binding of the headers in include/ -- argument marshalling only (cryptogen_requests.h: serving.py).
 
 Ciphertexts, keys and plaintexts are torch.int64 CUDA tensors whose bit
 patterns are the uint64 residues; every method passes data_ptr() values and
@@ -12,6 +12,7 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.environ.get("CRYPTOGEN_HIP_LIB", os.path.join(_HERE, "libcryptogen_hip.so"))
+_REQUESTS_PATH = os.environ.get("CRYPTOGEN_REQUESTS_LIB", os.path.join(_HERE, "libcryptogen_requests.so"))
 
 _SYMBOLS = [
     "cg_create", "cg_destroy", "cg_get_sizes", "cg_workspace_bytes", "cg_strerror",
@@ -25,6 +26,12 @@ _SYMBOLS = [
     "cg_rotate_hoisted", "cg_prefill_qk_hoisted", "cg_prefill_av_hoisted", "cg_cpvm_hoisted",
     "cg_rotate_sum_hoisted", "cg_round_galois", "cg_decode_scores_hoisted", "cg_decode_context_hoisted",
     "cg_decode_step_hoisted", "cg_mul_sum",
+]
+# libcryptogen_requests.so
+_REQUEST_SYMBOLS = [
+    "cg_req_create", "cg_req_destroy", "cg_slots_encode", "cg_slots_prepare", "cg_cpvm_diagonals",
+    "cg_cpvm_prepare_workspace_bytes", "cg_cpvm_prepare", "cg_cpvm_requests_workspace_bytes", "cg_cpvm_requests",
+    "cg_score_bias", "cg_prompt_bias", "cg_kv_append_requests",
 ]
 
 
@@ -45,8 +52,14 @@ class _KernelStat(C.Structure):
                 ("total_ms", C.c_double), ("algo_bytes", C.c_double), ("work_items", C.c_double)]
 
 
+def _params(params) -> _Params:
+    q = (C.c_uint64 * params.k)(*[int(x) for x in params.q])
+    p = (C.c_uint64 * params.nsp)(*[int(x) for x in params.p])
+    return _Params(params.log2n, params.k, params.nsp, params.alpha, int(params.t), q, p)
+
+
 class Library:
-    """The loaded shared library with typed entry points."""
+    """The loaded shared libraries with typed entry points."""
 
     def __init__(self, path: str = _LIB_PATH):
         if not os.path.exists(path):
@@ -118,6 +131,27 @@ class Library:
             if name not in ("cg_workspace_bytes", "cg_decode_step_workspace_bytes", "cg_strerror", "cg_kernel_name",
                             "cg_static_scratch_bytes"):
                 getattr(d, name).restype = i32
+        if not os.path.exists(_REQUESTS_PATH):
+            raise RuntimeError(f"{_REQUESTS_PATH} is missing: build it with `python -m paper_2602_08798_amd.build`")
+        # its entry points beside the evaluator's
+        r = self.requests_dll = C.CDLL(_REQUESTS_PATH)
+        for name in _REQUEST_SYMBOLS:
+            setattr(d, name, getattr(r, name))
+            getattr(d, name).restype = i32
+        d.cg_req_create.argtypes = [C.POINTER(vp), vp, C.POINTER(_Params)]
+        d.cg_req_destroy.argtypes = [vp]
+        d.cg_slots_encode.argtypes = d.cg_slots_prepare.argtypes = [vp, vp, vp, vp, u32]
+        d.cg_cpvm_diagonals.argtypes = [vp, u32, u32]
+        d.cg_cpvm_diagonals.restype = u32
+        d.cg_cpvm_prepare_workspace_bytes.argtypes = [vp, u32, u32, u32, u32]
+        d.cg_cpvm_prepare_workspace_bytes.restype = C.c_size_t
+        d.cg_cpvm_prepare.argtypes = [vp, vp, vp, vp, vp, u32, u32, u32, u32, u32, vp, vp]
+        d.cg_cpvm_requests_workspace_bytes.argtypes = [vp, u32, u32, u32]
+        d.cg_cpvm_requests_workspace_bytes.restype = C.c_size_t
+        d.cg_cpvm_requests.argtypes = [vp, vp, vp, vp, vp, u32, vp, u32, u32, u32, u32, u32, C.POINTER(vp), C.POINTER(vp), vp, vp]
+        d.cg_score_bias.argtypes = [vp, vp, vp, u32, u32, u32, u32, vp, vp, vp, u32, vp]
+        d.cg_prompt_bias.argtypes = [vp, vp, vp, u32, u32, u32, vp, vp, u32, vp]
+        d.cg_kv_append_requests.argtypes = [vp, vp, vp, u32, u32, u32, vp, vp, u32, vp, u32]
 
     def strerror(self, status: int) -> str:
         return self.dll.cg_strerror(status).decode()
@@ -134,7 +168,7 @@ def load_library() -> Library:
 
 
 def exported_symbols():
-    return list(_SYMBOLS)
+    return _SYMBOLS + _REQUEST_SYMBOLS
 
 
 def to_device(arr: np.ndarray, device="cuda") -> torch.Tensor:
@@ -190,9 +224,7 @@ class Context:
         self.n, self.k, self.nsp = params.n, params.k, params.nsp
         self.dnum = params.k // params.alpha
         self.L = self.k + self.nsp
-        q = (C.c_uint64 * self.k)(*[int(x) for x in params.q])
-        p = (C.c_uint64 * self.nsp)(*[int(x) for x in params.p])
-        prm = _Params(params.log2n, self.k, self.nsp, params.alpha, int(params.t), q, p)
+        prm = _params(params)
         h = C.c_void_p()
         with torch.cuda.device(self.device):
             self._check(self.lib.dll.cg_create(C.byref(h), C.byref(prm)))

@@ -1,4 +1,5 @@
-"""Compile the HIP library for gfx950 into paper_2602_08798_amd/libcryptogen_hip.so."""
+"""Compile the HIP libraries for gfx950 into paper_2602_08798_amd/: libcryptogen_hip.so, the evaluator, and
+libcryptogen_requests.so, which calls it."""
 import os
 import subprocess
 import sys
@@ -9,6 +10,10 @@ LIB = os.path.join(HERE, "libcryptogen_hip.so")
 DEPS = [SRC] + [os.path.join(HERE, "csrc", f) for f in ("kernels.hpp", "tables.hpp", "modarith.hpp")] + [
     os.path.join(os.path.dirname(HERE), "include", "cryptogen_bench.h"),
     os.path.join(os.path.dirname(HERE), "include", "cryptogen.h")]
+REQ_SRC = os.path.join(HERE, "csrc", "requests.hip")
+REQ_LIB = os.path.join(HERE, "libcryptogen_requests.so")
+REQ_DEPS = [REQ_SRC, LIB] + [os.path.join(HERE, "csrc", f) for f in ("requests.hpp", "kernels.hpp", "tables.hpp", "modarith.hpp")] + [
+    os.path.join(os.path.dirname(HERE), "include", f) for f in ("cryptogen_requests.h", "cryptogen.h")]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
@@ -18,12 +23,19 @@ FLAGS = [
 ]
 
 
+# The second library finds the first beside it, or as already loaded under this name.  Its kernels are its own: hidden.
+LINK = ["-Wl,-soname,libcryptogen_hip.so"]
+REQ_LINK = ["-fvisibility=hidden", "-Wl,-soname,libcryptogen_requests.so", "-L" + HERE, "-lcryptogen_hip", "-Wl,-rpath,$ORIGIN"]
+
+
+def _compile(src, lib, deps, force, extra):
+    if force or not os.path.exists(lib) or any(os.path.getmtime(lib) < os.path.getmtime(d) for d in deps):
+        subprocess.run(["hipcc"] + FLAGS + ["-o", lib, src] + extra, check=True)
+
+
 def build(force: bool = True, extra=()) -> str:
-    if not force and os.path.exists(LIB) and all(
-            os.path.getmtime(LIB) >= os.path.getmtime(d) for d in DEPS):
-        return LIB
-    cmd = ["hipcc"] + FLAGS + list(extra) + ["-o", LIB, SRC]
-    subprocess.run(cmd, check=True)
+    _compile(SRC, LIB, DEPS, force, LINK + list(extra))
+    _compile(REQ_SRC, REQ_LIB, REQ_DEPS, force, REQ_LINK + list(extra))
     return LIB
 
 

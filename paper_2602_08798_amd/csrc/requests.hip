@@ -1,0 +1,413 @@
+// libcryptogen_requests.so (see include/cryptogen_requests.h): tables, argument checks and launch sequences.
+// Rotations go through the evaluator's public entry points.
+#include "../../include/cryptogen_requests.h"
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstring>
+#include <initializer_list>
+#include <new>
+#include <tuple>
+#include <vector>
+
+// the row transforms are this library's own copies: nothing of them is exported beside the evaluator's
+namespace {
+#include "requests.hpp"
+}
+using namespace cgr;
+
+#define CG_REQUIRE(cond) do { if (!(cond)) return CG_EINVAL; } while (0)
+#define CG_TRY(expr) do { int rc_ = (expr); if (rc_ != CG_OK) return rc_; } while (0)
+#define CG_API extern "C" __attribute__((visibility("default")))
+
+struct cg_req {
+    cg_ctx *ctx;
+    int logn, N, k, nsp, device, n_cu;
+    void *mem;            // every table
+    Tables T;
+};
+
+namespace {
+typedef unsigned __int128 u128;
+uint64_t mul_mod(uint64_t a, uint64_t b, uint64_t m) { return (uint64_t)((u128)a * b % m); }
+uint64_t pow_mod(uint64_t a, uint64_t e, uint64_t m)
+{
+    uint64_t r = 1;
+    for (a %= m; e; e >>= 1, a = mul_mod(a, a, m))
+        if (e & 1) r = mul_mod(r, a, m);
+    return r;
+}
+uint64_t inverse_mod(uint64_t a, uint64_t m) { return pow_mod(a, m - 2, m); }
+double centred(uint64_t x, uint64_t m) { return x > m / 2 ? -(double)(m - x) : (double)x; }
+bool small_prime(uint64_t n)
+{
+    if (n < 3 || n % 2 == 0) return false;
+    for (uint64_t d = 3; d * d <= n; d += 2)
+        if (n % d == 0) return false;
+    return true;
+}
+// the smallest primitive 2n-th root of unity modulo the prime p = 1 mod 2n (n a power of two); 0: none found
+uint64_t smallest_root(uint64_t n, uint64_t p)
+{
+    for (uint64_t g = 2; g < 2000; g++) {
+        const uint64_t r = pow_mod(g, (p - 1) / (2 * n), p);
+        if (pow_mod(r, n, p) != p - 1) continue;
+        uint64_t best = r, cur = r;
+        const uint64_t sq = mul_mod(r, r, p);
+        for (uint64_t i = 1; i < n; i++) {
+            cur = mul_mod(cur, sq, p);
+            best = std::min(best, cur);
+        }
+        return best;
+    }
+    return 0;
+}
+uint32_t reversed(uint32_t x, int bits)
+{
+    uint32_t r = 0;
+    for (int i = 0; i < bits; i++) r |= ((x >> i) & 1) << (bits - 1 - i);
+    return r;
+}
+bool aligned(const void *p, uintptr_t to = 16) { return p && (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
+bool all_aligned(std::initializer_list<const void *> ps)
+{
+    for (const void *p : ps) if (!aligned(p)) return false;
+    return true;
+}
+bool overlap(const void *a, size_t na, const void *b, size_t nb)
+{
+    const char *x = static_cast<const char *>(a), *y = static_cast<const char *>(b);
+    return x < y + nb && y < x + na;
+}
+bool power_of_two(uint32_t x) { return x && !(x & (x - 1)); }
+int log2_of(uint32_t x) { int l = 0; while (x >>= 1) l++; return l; }
+bool in_one_call(uint64_t units) { return units >= 1 && units <= (1u << 16); }
+bool here(const cg_req *c)
+{
+    int d;
+    return hipGetDevice(&d) == hipSuccess && d == c->device;
+}
+size_t row_bytes(const cg_req *c) { return (size_t)c->N * 8; }
+size_t ct_bytes(const cg_req *c) { return 2 * (size_t)c->k * row_bytes(c); }
+
+// the launch's own status: an error that other code left pending in the thread is neither reported as ours nor cleared
+template <class... P, class... A>
+int launch(void (*kernel)(P...), dim3 grid, unsigned block, size_t lds, void *s, A... args)
+{
+    std::tuple<P...> pack{static_cast<P>(args)...};
+    void *ptrs[sizeof...(P)];
+    int i = 0;
+    std::apply([&](auto &...e) { ((ptrs[i++] = static_cast<void *>(&e)), ...); }, pack);
+    return hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(block), ptrs, lds, static_cast<hipStream_t>(s)) == hipSuccess
+               ? CG_OK : CG_EHIP;
+}
+// KERNEL<LOGN, E, ...> for the handle's ring, a row to a workgroup
+#define CG_ROWS(c, rows, s, KERNEL, MORE, ...)                                                              \
+    ((c)->logn == 12 ? launch(KERNEL<12, 8 MORE>, dim3((unsigned)(rows)), 512, 0, s, __VA_ARGS__)                 \
+     : (c)->logn == 13 ? launch(KERNEL<13, 8 MORE>, dim3((unsigned)(rows)), 1024, 0, s, __VA_ARGS__)              \
+                       : launch(KERNEL<14, 16 MORE>, dim3((unsigned)(rows)), 1024, 0, s, __VA_ARGS__))
+#define CG_COMMA ,
+
+int create(cg_req *c, const cg_params *prm)
+{
+    const int logn = c->logn, k = c->k;
+    const size_t N = c->N;
+    uint64_t pr[MAXPR];
+    for (int i = 0; i < k; i++) pr[i] = prm->q[i];
+    pr[k] = prm->t;
+    DevConst H;
+    memset(&H, 0, sizeof(H));
+    H.logn = logn; H.k = k; H.nsp = c->nsp; H.np = k + 1; H.tmod = (double)prm->t;
+    std::vector<double> tw((k + 1) * N), itw((k + 1) * N);
+    std::vector<uint16_t> slot(N), pow3(N / 2);
+    std::vector<float> zeta(2 * N);
+    std::vector<uint64_t> pw(2 * N);
+    for (int r = 0; r <= k; r++) {
+        const uint64_t p = pr[r], psi = smallest_root(N, p), ninv = inverse_mod(N % p, p);
+        CG_REQUIRE(psi);
+        H.mod[r].p = (double)p;
+        H.mod[r].u = 1.0 / (double)p;
+        pw[0] = 1;
+        for (size_t i = 1; i < 2 * N; i++) pw[i] = mul_mod(pw[i - 1], psi, p);
+        for (size_t j = 0; j < N; j++) {
+            const uint32_t e = reversed((uint32_t)j, logn);
+            tw[r * N + j] = centred(pw[e], p);
+            itw[r * N + j] = centred(pw[(2 * N - e) % (2 * N)], p);
+        }
+        H.ninv[r] = centred(ninv, p);
+        H.itw1_ninv[r] = centred(mul_mod(pw[2 * N - reversed(1, logn)], ninv, p), p);
+    }
+    // (pw now holds the powers of zeta)
+    for (size_t e = 0; e < 2 * N; e++) zeta[e] = (float)centred(pw[e], prm->t);
+    uint32_t e = 1;
+    for (size_t i = 0; i < N / 2; i++, e = e * 3 % (2 * (uint32_t)N)) {
+        pow3[i] = (uint16_t)e;
+        slot[reversed((e - 1) / 2, logn)] = (uint16_t)i;
+        slot[reversed((2 * (uint32_t)N - e - 1) / 2, logn)] = (uint16_t)(N / 2 + i);
+    }
+    // floor(Q / t) = -(Q mod t) / t modulo q_i
+    uint64_t q_mod_t = 1;
+    for (int i = 0; i < k; i++) q_mod_t = mul_mod(q_mod_t, pr[i] % prm->t, prm->t);
+    for (int i = 0; i < k; i++) H.delta_q[i] = centred(mul_mod(pr[i] - q_mod_t, inverse_mod(prm->t, pr[i]), pr[i]), pr[i]);
+
+    const size_t parts[] = {sizeof(DevConst), tw.size() * 8, itw.size() * 8, slot.size() * 2, zeta.size() * 4, pow3.size() * 2};
+    const void *from[] = {&H, tw.data(), itw.data(), slot.data(), zeta.data(), pow3.data()};
+    char *to[6];
+    size_t total = 0;
+    for (size_t n : parts) total += (n + 255) / 256 * 256;
+    if (hipMalloc(&c->mem, total) != hipSuccess) {
+        c->mem = nullptr;
+        return CG_ENOMEM;
+    }
+    char *at = static_cast<char *>(c->mem);
+    for (int i = 0; i < 6; i++) {
+        to[i] = at;
+        if (hipMemcpy(at, from[i], parts[i], hipMemcpyHostToDevice) != hipSuccess) return CG_EHIP;
+        at += (parts[i] + 255) / 256 * 256;
+    }
+    c->T = Tables{reinterpret_cast<DevConst *>(to[0]), reinterpret_cast<double *>(to[1]), reinterpret_cast<double *>(to[2]),
+                  reinterpret_cast<uint16_t *>(to[3]), reinterpret_cast<float *>(to[4]), reinterpret_cast<uint16_t *>(to[5]),
+                  H.ninv[k], logn, k};
+    return hipDeviceSynchronize() == hipSuccess ? CG_OK : CG_EHIP;
+}
+
+template <bool PREPARED, class LD>
+int encode(const cg_req *c, void *s, LD ld, void *out, uint32_t batch)
+{
+    const int split = 1;
+    return CG_ROWS(c, (size_t)batch * split, s, encode_kernel, CG_COMMA PREPARED CG_COMMA LD, ld, out, c->T, split);
+}
+
+// generators of the sum over residue classes modulo d2: rotations by d2, 2 d2, ... N/4, then the row swap
+int fold_bits(const cg_req *c, uint32_t d2) { return c->logn - 2 - log2_of(d2) + 2; }
+}  // namespace
+
+CG_API int cg_req_create(cg_req **out, cg_ctx *ctx, const cg_params *prm)
+{
+    CG_REQUIRE(out);
+    *out = nullptr;
+    CG_REQUIRE(ctx && prm && prm->q && prm->log2n >= 12 && prm->log2n <= 14 && prm->k >= 1 && prm->k <= 6 && prm->nsp >= 1 &&
+               prm->nsp <= 2 && prm->alpha >= 1 && prm->k % prm->alpha == 0);
+    const uint64_t N = 1ull << prm->log2n;
+    CG_REQUIRE(prm->t < (1u << 20) && prm->t % (2 * N) == 1 && small_prime(prm->t));
+    for (uint32_t i = 0; i < prm->k; i++) CG_REQUIRE(prm->q[i] % (2 * N) == 1 && prm->q[i] > (1ull << 40) && prm->q[i] < (1ull << 50));
+    // the context has these sizes
+    cg_sizes z;
+    CG_TRY(cg_get_sizes(ctx, &z));
+    CG_REQUIRE(z.ct2_bytes == 2 * prm->k * N * 8 && z.ksk_raw_bytes == (size_t)(prm->k / prm->alpha) * 2 * (prm->k + prm->nsp) * N * 8);
+    cg_req *c = new (std::nothrow) cg_req();
+    if (!c) return CG_ENOMEM;
+    c->ctx = ctx;
+    c->logn = (int)prm->log2n; c->N = (int)N; c->k = (int)prm->k; c->nsp = (int)prm->nsp;
+    int rc = CG_EHIP;
+    if (hipGetDevice(&c->device) == hipSuccess &&
+        hipDeviceGetAttribute(&c->n_cu, hipDeviceAttributeMultiprocessorCount, c->device) == hipSuccess && c->n_cu >= 1) {
+        try {
+            rc = create(c, prm);
+        } catch (const std::bad_alloc &) {
+            rc = CG_ENOMEM;
+        }
+    }
+    if (rc != CG_OK) {
+        if (c->mem) (void)hipFree(c->mem);
+        delete c;
+        return rc;
+    }
+    *out = c;
+    return CG_OK;
+}
+
+CG_API int cg_req_destroy(cg_req *c)
+{
+    if (!c) return CG_OK;
+    (void)hipDeviceSynchronize();
+    if (c->mem) (void)hipFree(c->mem);
+    delete c;
+    return CG_OK;
+}
+
+CG_API int cg_slots_encode(cg_req *c, void *stream, const int64_t *slots, uint64_t *pt, uint32_t batch)
+{
+    CG_REQUIRE(c && all_aligned({slots, pt}) && in_one_call(batch) && here(c));
+    CG_REQUIRE(!overlap(slots, row_bytes(c) * batch, pt, row_bytes(c) * batch));
+    return encode<false>(c, stream, LdSlots{slots, c->logn}, pt, batch);
+}
+
+CG_API int cg_slots_prepare(cg_req *c, void *stream, const int64_t *slots, void *plain, uint32_t batch)
+{
+    CG_REQUIRE(c && all_aligned({slots, plain}) && in_one_call(batch) && here(c));
+    CG_REQUIRE(!overlap(slots, row_bytes(c) * batch, plain, row_bytes(c) * c->k * batch));
+    return encode<true>(c, stream, LdSlots{slots, c->logn}, plain, batch);
+}
+
+// ---------------------------------------------------------------------------
+// projections
+// ---------------------------------------------------------------------------
+static bool block_length_ok(const cg_req *c, uint32_t d2) { return power_of_two(d2) && d2 >= 2 && d2 <= (uint32_t)c->N / 4; }
+static uint32_t tile_length(const cg_req *c, uint32_t d1, uint32_t d2)
+{
+    uint32_t tile = std::max(d2, (uint32_t)c->N / d2);
+    while (tile < d1) tile *= 2;
+    return tile;
+}
+
+CG_API uint32_t cg_cpvm_diagonals(const cg_req *c, uint32_t d1, uint32_t d2)
+{
+    if (!c || !block_length_ok(c, d2) || d1 < 1 || d1 > (uint32_t)c->N / 2) return 0;
+    const uint32_t tile = tile_length(c, d1, d2);
+    if (tile > (uint32_t)c->N / 2) return 0;
+    const uint64_t n_diag = (uint64_t)d2 * tile / c->N;
+    return n_diag <= 64 ? (uint32_t)n_diag : 0;
+}
+
+CG_API size_t cg_cpvm_prepare_workspace_bytes(const cg_req *c, uint32_t units, uint32_t d1, uint32_t d2, uint32_t rank)
+{
+    if (!rank || !cg_cpvm_diagonals(c, d1, d2)) return 0;
+    return (size_t)units * d1 * d2 * sizeof(float);
+}
+
+CG_API int cg_cpvm_prepare(cg_req *c, void *stream, const int64_t *w, const int64_t *a, const int64_t *b, uint32_t units,
+                           uint32_t a_group, uint32_t d1, uint32_t d2, uint32_t rank, void *diags, void *ws)
+{
+    const uint32_t n_diag = cg_cpvm_diagonals(c, d1, d2);
+    CG_REQUIRE(n_diag && units >= 1 && in_one_call((uint64_t)units * n_diag) && aligned(diags) && here(c));
+    CG_REQUIRE(rank ? rank <= 4096 && a_group >= 1 && all_aligned({a, b, ws}) && (!w || aligned(w)) : !a && !b && aligned(w));
+    const size_t out = row_bytes(c) * c->k * n_diag * units, mats = (size_t)units * d1 * d2;
+    const int log_tile = log2_of(tile_length(c, d1, d2)), log_diag = log2_of(n_diag), log_d2 = log2_of(d2);
+    CG_REQUIRE(!w || !overlap(w, mats * 8, diags, out));
+    if (!rank) return encode<true>(c, stream, LdDiagonal<int64_t>{w, c->logn, log_tile, log_diag, log_d2, (int)d1}, diags, units * n_diag);
+    const size_t na = (size_t)((units - 1) / a_group + 1) * d1 * rank * 8, nb = (size_t)units * rank * d2 * 8;
+    for (const void *p : {diags, ws}) {
+        const size_t n = p == diags ? out : mats * sizeof(float);
+        CG_REQUIRE(!overlap(a, na, p, n) && !overlap(b, nb, p, n) && (!w || !overlap(w, mats * 8, p, n)));
+    }
+    CG_REQUIRE(!overlap(ws, mats * sizeof(float), diags, out));
+    const uint32_t row_blocks = (d1 + 63) / 64;
+    float *m = static_cast<float *>(ws);
+    CG_TRY(launch(low_rank_kernel, dim3(units * row_blocks, (d2 + 63) / 64), 256, 0, stream, w, a, b, m, (int)a_group, (int)d1, (int)d2,
+                  (int)rank, (int)row_blocks, c->T));
+    return encode<true>(c, stream, LdDiagonal<float>{m, c->logn, log_tile, log_diag, log_d2, (int)d1}, diags, units * n_diag);
+}
+
+CG_API size_t cg_cpvm_requests_workspace_bytes(const cg_req *c, uint32_t requests, uint32_t units, uint32_t n_diag)
+{
+    if (!c || !in_one_call((uint64_t)requests * units) || !n_diag || n_diag > 64 || !in_one_call((uint64_t)requests * n_diag)) return 0;
+    const size_t copies = n_diag - 1, cts = requests * copies + (size_t)requests * n_diag + 2 * (size_t)requests * units;
+    const size_t series = copies ? cg_workspace_bytes(c->ctx, (uint32_t)(requests * copies + requests)) : 0;
+    return cts * ct_bytes(c) + std::max(series, cg_workspace_bytes(c->ctx, requests * units));
+}
+
+static int cpvm_requests(cg_req *c, void *stream, const uint64_t *x, const void *diags, const void *adapters, uint32_t n_adapters,
+                         const int32_t *pick, uint32_t requests, uint32_t units, uint32_t n_diag, uint32_t d2,
+                         uint32_t round_bits, const void *const *gk_copies, const void *const *gk_block, uint64_t *out, void *ws)
+{
+    const uint32_t batch = requests * units;
+    const size_t ct = ct_bytes(c);
+    // the rounds of the sum over residue classes, or one generator after the other
+    const int bits = fold_bits(c, d2);
+    std::vector<uint32_t> elts, counts;
+    if (round_bits) {
+        const int rounds = (bits + (int)round_bits - 1) / (int)round_bits, lo = bits / rounds, extra = bits % rounds;
+        for (int r = 0; r < rounds; r++) counts.push_back((1u << (lo + (r < extra))) - 1);
+    } else {
+        counts.assign(bits, 1);
+    }
+    uint32_t n_keys = 0;
+    CG_TRY(cg_round_galois(c->ctx, 1, d2, round_bits ? round_bits : 1, nullptr, 0, &n_keys));
+    elts.resize(n_keys);
+    CG_TRY(cg_round_galois(c->ctx, 1, d2, round_bits ? round_bits : 1, elts.data(), n_keys, &n_keys));
+    uint32_t total = 0;
+    for (uint32_t n : counts) total += n;
+    CG_REQUIRE(total == n_keys);
+    for (uint32_t i = 0; i < n_keys; i++) CG_REQUIRE(aligned(gk_block[i]));
+
+    char *at = static_cast<char *>(ws);
+    auto take = [&](size_t cts) { char *p = at; at += cts * ct; return p; };
+    uint64_t *copies = reinterpret_cast<uint64_t *>(take((size_t)requests * (n_diag - 1)));
+    double *f = reinterpret_cast<double *>(take((size_t)requests * n_diag));
+    uint64_t *xa = reinterpret_cast<uint64_t *>(take(batch)), *xb = reinterpret_cast<uint64_t *>(take(batch));
+    void *rest = at;
+    if (n_diag > 1) {
+        uint32_t gs[64], e = 1;
+        for (uint32_t i = 1; i < n_diag; i++) gs[i - 1] = e = e * 3 % (2u * (uint32_t)c->N);
+        CG_TRY(cg_rotate_hoisted(c->ctx, stream, x, n_diag - 1, gs, gk_copies, copies, requests, rest));
+    }
+    CG_TRY(CG_ROWS(c, (size_t)requests * n_diag * 2 * c->k, stream, copies_kernel, , x, copies, f, (int)n_diag, c->T));
+    CG_TRY(CG_ROWS(c, (size_t)batch * 2 * c->k, stream, project_kernel, , f, static_cast<const double *>(diags),
+                   static_cast<const double *>(adapters), (int)n_adapters, pick, (int)units, (int)n_diag, xa, c->T));
+    uint64_t *cur = xa, *next = xb;
+    for (size_t r = 0, first = 0; r < counts.size(); first += counts[r], r++) {
+        uint64_t *to = r + 1 == counts.size() ? out : next;
+        if (round_bits) CG_TRY(cg_rotate_sum_hoisted(c->ctx, stream, cur, counts[r], elts.data() + first, gk_block + first, to, batch, rest));
+        else CG_TRY(cg_rotate(c->ctx, stream, cur, elts[first], gk_block[first], to, batch, 1, rest));
+        next = cur;
+        cur = to;
+    }
+    return CG_OK;
+}
+
+CG_API int cg_cpvm_requests(cg_req *c, void *stream, const uint64_t *x, const void *diags, const void *adapters, uint32_t n_adapters,
+                            const int32_t *pick, uint32_t requests, uint32_t units, uint32_t n_diag, uint32_t d2,
+                            uint32_t round_bits, const void *const *gk_copies, const void *const *gk_block, uint64_t *out, void *ws)
+{
+    CG_REQUIRE(c && all_aligned({x, diags, out, ws}) && requests >= 1 && units >= 1 && in_one_call((uint64_t)requests * units));
+    CG_REQUIRE(block_length_ok(c, d2) && power_of_two(n_diag) && n_diag <= 64 && n_diag <= d2 && in_one_call((uint64_t)requests * n_diag));
+    CG_REQUIRE(n_adapters ? aligned(adapters) && aligned(pick, 4) && n_adapters < (1u << 31) : !adapters);
+    CG_REQUIRE(round_bits <= 7 && gk_block && (n_diag == 1 || gk_copies) && here(c));
+    for (uint32_t i = 0; i + 1 < n_diag; i++) CG_REQUIRE(aligned(gk_copies[i]));
+    const size_t n_ws = cg_cpvm_requests_workspace_bytes(c, requests, units, n_diag), n_out = ct_bytes(c) * requests * units;
+    CG_REQUIRE(!overlap(x, ct_bytes(c) * requests, out, n_out) && !overlap(ws, n_ws, out, n_out) && !overlap(ws, n_ws, x, ct_bytes(c) * requests));
+    try {
+        return cpvm_requests(c, stream, x, diags, adapters, n_adapters, pick, requests, units, n_diag, d2, round_bits, gk_copies, gk_block,
+                             out, ws);
+    } catch (const std::bad_alloc &) {
+        return CG_ENOMEM;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// position biases
+// ---------------------------------------------------------------------------
+static int add_bias(cg_req *c, void *stream, const uint64_t *in, uint32_t groups, uint32_t heads, uint32_t n_cts, uint32_t d2,
+                    const int32_t *pos, const int64_t *table, const int32_t *edges, uint32_t n_buckets, uint64_t *out)
+{
+    CG_REQUIRE(c && all_aligned({in, out, table}) && aligned(edges, 4) && block_length_ok(c, d2) && here(c));
+    CG_REQUIRE(groups >= 1 && heads >= 1 && n_cts >= 1 && n_buckets >= 1 && n_buckets <= 4096);
+    CG_REQUIRE(in_one_call((uint64_t)groups * heads) && in_one_call((uint64_t)groups * heads * n_cts));
+    const uint32_t units = groups * heads * n_cts;
+    CG_REQUIRE(in == out || !overlap(in, ct_bytes(c) * units, out, ct_bytes(c) * units));
+    const int parts = 4;
+    const BiasArgs A{in, out, pos, table, edges, (int)n_buckets, (int)heads, (int)n_cts, log2_of(d2), parts};
+    return launch(bias_kernel, dim3(units * parts), BIAS_THREADS, (size_t)c->N / d2 * sizeof(float), stream, A, c->T);
+}
+
+CG_API int cg_score_bias(cg_req *c, void *stream, const uint64_t *scores, uint32_t requests, uint32_t heads, uint32_t n_cts, uint32_t d2,
+                         const int32_t *pos, const int64_t *table, const int32_t *edges, uint32_t n_buckets, uint64_t *out)
+{
+    CG_REQUIRE(aligned(pos, 4));
+    return add_bias(c, stream, scores, requests, heads, n_cts, d2, pos, table, edges, n_buckets, out);
+}
+
+CG_API int cg_prompt_bias(cg_req *c, void *stream, const uint64_t *diags, uint32_t prompts, uint32_t heads, uint32_t d2,
+                          const int64_t *table, const int32_t *edges, uint32_t n_buckets, uint64_t *out)
+{
+    CG_REQUIRE(c && block_length_ok(c, d2));
+    return add_bias(c, stream, diags, prompts, heads, (uint32_t)c->N / d2, d2, nullptr, table, edges, n_buckets, out);
+}
+
+// ---------------------------------------------------------------------------
+// appends
+// ---------------------------------------------------------------------------
+CG_API int cg_kv_append_requests(cg_req *c, void *stream, uint64_t *cache, uint32_t cache_stride_cts, uint32_t requests, uint32_t per,
+                                 const int32_t *lens, const uint64_t *rows, uint32_t row_stride_cts, const void *masks, uint32_t d2)
+{
+    CG_REQUIRE(c && all_aligned({cache, rows, masks}) && aligned(lens, 4) && here(c));
+    CG_REQUIRE(requests >= 1 && per >= 1 && in_one_call((uint64_t)requests * per) && cache_stride_cts >= 1 && row_stride_cts >= per);
+    CG_REQUIRE(power_of_two(d2) && d2 <= (uint32_t)c->N / 2);
+    const size_t caches = (size_t)requests * per, n_rows = ((size_t)(requests - 1) * row_stride_cts + per) * ct_bytes(c);
+    CG_REQUIRE(!overlap(cache, caches * cache_stride_cts * ct_bytes(c), rows, n_rows));
+    const AppendArgs A{cache, rows, static_cast<const double *>(masks), lens, (int)per, log2_of((uint32_t)c->N / d2), cache_stride_cts,
+                       row_stride_cts};
+    return CG_ROWS(c, caches * 2 * c->k, stream, append_kernel, , A, c->T);
+}
