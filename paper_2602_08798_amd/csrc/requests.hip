@@ -102,12 +102,16 @@ int launch(void (*kernel)(P...), dim3 grid, unsigned block, size_t lds, void *s,
     return hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(block), ptrs, lds, static_cast<hipStream_t>(s)) == hipSuccess
                ? CG_OK : CG_EHIP;
 }
-// KERNEL<LOGN, E, ...> for the handle's ring, a row to a workgroup
-#define CG_ROWS(c, rows, s, KERNEL, MORE, ...)                                                              \
-    ((c)->logn == 12 ? launch(KERNEL<12, 8 MORE>, dim3((unsigned)(rows)), 512, 0, s, __VA_ARGS__)                 \
-     : (c)->logn == 13 ? launch(KERNEL<13, 8 MORE>, dim3((unsigned)(rows)), 1024, 0, s, __VA_ARGS__)              \
-                       : launch(KERNEL<14, 16 MORE>, dim3((unsigned)(rows)), 1024, 0, s, __VA_ARGS__))
-#define CG_COMMA ,
+// KERNEL<LOGN, E, more> of ARGS for the handle's ring, a row to a workgroup.  WIDE: N = 8192 on 512 threads, two workgroups to a
+// compute unit
+#define CG_LIST(...) __VA_ARGS__
+#define CG_ROWS_OF(c, rows, s, WIDE, ARGS, KERNEL, ...)                                                                                     \
+    ((c)->logn == 12 ? launch(KERNEL<12, 8 __VA_OPT__(, ) __VA_ARGS__>, dim3((unsigned)(rows)), 512, 0, s, CG_LIST ARGS)                   \
+     : (c)->logn == 14 ? launch(KERNEL<14, 16 __VA_OPT__(, ) __VA_ARGS__>, dim3((unsigned)(rows)), 1024, 0, s, CG_LIST ARGS)               \
+                       : launch(KERNEL<13, WIDE ? 16 : 8 __VA_OPT__(, ) __VA_ARGS__>, dim3((unsigned)(rows)), WIDE ? 512 : 1024, 0, s,     \
+                                CG_LIST ARGS))
+#define CG_ROWS(c, rows, s, ...) CG_ROWS_OF(c, rows, s, false, __VA_ARGS__)
+#define CG_ROWS_WIDE(c, rows, s, ...) CG_ROWS_OF(c, rows, s, true, __VA_ARGS__)
 
 int create(cg_req *c, const cg_params *prm)
 {
@@ -120,7 +124,7 @@ int create(cg_req *c, const cg_params *prm)
     memset(&H, 0, sizeof(H));
     H.logn = logn; H.k = k; H.nsp = c->nsp; H.np = k + 1; H.tmod = (double)prm->t;
     std::vector<double> tw((k + 1) * N), itw((k + 1) * N);
-    std::vector<uint16_t> slot(N), pow3(N / 2);
+    std::vector<uint16_t> place(N), pow3(N / 2);
     std::vector<float> zeta(2 * N);
     std::vector<uint64_t> pw(2 * N);
     for (int r = 0; r <= k; r++) {
@@ -143,16 +147,16 @@ int create(cg_req *c, const cg_params *prm)
     uint32_t e = 1;
     for (size_t i = 0; i < N / 2; i++, e = e * 3 % (2 * (uint32_t)N)) {
         pow3[i] = (uint16_t)e;
-        slot[reversed((e - 1) / 2, logn)] = (uint16_t)i;
-        slot[reversed((2 * (uint32_t)N - e - 1) / 2, logn)] = (uint16_t)(N / 2 + i);
+        place[i] = (uint16_t)reversed((e - 1) / 2, logn);
+        place[N / 2 + i] = (uint16_t)reversed((2 * (uint32_t)N - e - 1) / 2, logn);
     }
     // floor(Q / t) = -(Q mod t) / t modulo q_i
     uint64_t q_mod_t = 1;
     for (int i = 0; i < k; i++) q_mod_t = mul_mod(q_mod_t, pr[i] % prm->t, prm->t);
     for (int i = 0; i < k; i++) H.delta_q[i] = centred(mul_mod(pr[i] - q_mod_t, inverse_mod(prm->t, pr[i]), pr[i]), pr[i]);
 
-    const size_t parts[] = {sizeof(DevConst), tw.size() * 8, itw.size() * 8, slot.size() * 2, zeta.size() * 4, pow3.size() * 2};
-    const void *from[] = {&H, tw.data(), itw.data(), slot.data(), zeta.data(), pow3.data()};
+    const size_t parts[] = {sizeof(DevConst), tw.size() * 8, itw.size() * 8, place.size() * 2, zeta.size() * 4, pow3.size() * 2};
+    const void *from[] = {&H, tw.data(), itw.data(), place.data(), zeta.data(), pow3.data()};
     char *to[6];
     size_t total = 0;
     for (size_t n : parts) total += (n + 255) / 256 * 256;
@@ -172,11 +176,42 @@ int create(cg_req *c, const cg_params *prm)
     return hipDeviceSynchronize() == hipSuccess ? CG_OK : CG_EHIP;
 }
 
+// Prepared plaintexts of a last round that leaves compute units free are shared by several workgroups, which repeat the interpolation and
+// divide the primes (at N = 4096, where several workgroups fit a unit, only where no round is full).  us, a workgroup each / shared, N = 8192: 1
+// 22.5 / 12.9, 85 24.7 / 16.3, 128 25.5 / 21.6, 288 47.7 / 38.5, 341 48.5 / 41.1; N = 4096: 1 10.2 / 7.8, 128 11.6 / 9.3, 300 17.9 / 17.9; N = 16384: 1
+// 72.9 / 24.1, 86 76.5 / 48.6, 300 157 / 120.  From a full round on rows of 8192 take 512 threads: 288 38.6 / 35.0, 512 52.2 / 48.5, 1000 103 / 95.7
+// (below, 128 23.5 / 25.4).
 template <bool PREPARED, class LD>
 int encode(const cg_req *c, void *s, LD ld, void *out, uint32_t batch)
 {
-    const int split = 1;
-    return CG_ROWS(c, (size_t)batch * split, s, encode_kernel, CG_COMMA PREPARED CG_COMMA LD, ld, out, c->T, split);
+    const int cu = c->n_cu, rest = (int)batch % cu;
+    int whole = (int)batch, split = 1;
+    if (PREPARED && rest && ((int)batch < cu || c->logn > 12)) {
+        const int most = std::min(c->k, cu / rest), each = (c->k + most - 1) / most;      // primes a workgroup
+        split = (c->k + each - 1) / each;
+        whole -= rest;
+    }
+    const int grid = whole + ((int)batch - whole) * split;
+    if constexpr (PREPARED)
+        if ((int)batch > cu) return CG_ROWS_WIDE(c, grid, s, (ld, out, c->T, whole, split), encode_kernel, PREPARED, LD);
+    return CG_ROWS(c, grid, s, (ld, out, c->T, whole, split), encode_kernel, PREPARED, LD);
+}
+
+// How many of the ciphertexts that are left go through their rounds together, at N = 8192: whole rounds of the compute units first.  The evaluator
+// takes a unit's key switch on one workgroup where the last round of units is nine tenths full, and the (unit, prime) rows where theirs
+// is nearly full; with a few units more than that, every launch of the whole call is of the slower kind.  us a round of 7 / 3
+// rotations, in one call and with whole rounds first: 576 units 703 / 558 and 594 / 473, 540 680 / 544 and 570 / 461, 700 852 / 585 and 745 / 596,
+// 320 399 / 318 and 377 / 266, 288 377 / 302 and 361 / 259, 144 224 / 181 and 185 / 144, 72 120 / 98 and 113 / 92; beyond the limits 200 265 / 210
+// and 260 / 207, 108 130 / 102 and 153 / 117.  (N = 4096: 576 units 187 / 151 and 179 / 138, 300 106 / 84 and 111 / 91; N = 16384: 40 292 / 239 and 275 / 230,
+// 96 and more even: left whole.)
+uint32_t fold_together(const cg_req *c, uint32_t left)
+{
+    const uint32_t cu = (uint32_t)c->n_cu, rest = left % cu;
+    if (c->logn != 13) return left;
+    if (left >= cu) return 10 * rest >= 9 * cu ? left : left - rest;
+    if (2 * left > cu && 8 * left <= 5 * cu) return cu / 2;
+    if (4 * left > cu && 5 * left <= 2 * cu) return cu / 4;
+    return left;
 }
 
 // generators of the sum over residue classes modulo d2: rotations by d2, 2 d2, ... N/4, then the row swap
@@ -264,7 +299,7 @@ CG_API uint32_t cg_cpvm_diagonals(const cg_req *c, uint32_t d1, uint32_t d2)
 CG_API size_t cg_cpvm_prepare_workspace_bytes(const cg_req *c, uint32_t units, uint32_t d1, uint32_t d2, uint32_t rank)
 {
     if (!rank || !cg_cpvm_diagonals(c, d1, d2)) return 0;
-    return (size_t)units * d1 * d2 * sizeof(float);
+    return (size_t)units * tile_length(c, d1, d2) * d2 * sizeof(float);
 }
 
 CG_API int cg_cpvm_prepare(cg_req *c, void *stream, const int64_t *w, const int64_t *a, const int64_t *b, uint32_t units,
@@ -273,21 +308,22 @@ CG_API int cg_cpvm_prepare(cg_req *c, void *stream, const int64_t *w, const int6
     const uint32_t n_diag = cg_cpvm_diagonals(c, d1, d2);
     CG_REQUIRE(n_diag && units >= 1 && in_one_call((uint64_t)units * n_diag) && aligned(diags) && here(c));
     CG_REQUIRE(rank ? rank <= 4096 && a_group >= 1 && all_aligned({a, b, ws}) && (!w || aligned(w)) : !a && !b && aligned(w));
-    const size_t out = row_bytes(c) * c->k * n_diag * units, mats = (size_t)units * d1 * d2;
-    const int log_tile = log2_of(tile_length(c, d1, d2)), log_diag = log2_of(n_diag), log_d2 = log2_of(d2);
-    CG_REQUIRE(!w || !overlap(w, mats * 8, diags, out));
-    if (!rank) return encode<true>(c, stream, LdDiagonal<int64_t>{w, c->logn, log_tile, log_diag, log_d2, (int)d1}, diags, units * n_diag);
+    const uint32_t tile = tile_length(c, d1, d2);
+    const size_t out = row_bytes(c) * c->k * n_diag * units, mats = (size_t)units * d1 * d2 * 8, skewed = (size_t)units * tile * d2 * sizeof(float);
+    const Diagonal D{c->logn, log2_of(tile), log2_of(n_diag), log2_of(d2), (int)d1};
+    CG_REQUIRE(!w || !overlap(w, mats, diags, out));
+    if (!rank) return encode<true>(c, stream, LdMatrix{D, w}, diags, units * n_diag);
     const size_t na = (size_t)((units - 1) / a_group + 1) * d1 * rank * 8, nb = (size_t)units * rank * d2 * 8;
     for (const void *p : {diags, ws}) {
-        const size_t n = p == diags ? out : mats * sizeof(float);
-        CG_REQUIRE(!overlap(a, na, p, n) && !overlap(b, nb, p, n) && (!w || !overlap(w, mats * 8, p, n)));
+        const size_t n = p == diags ? out : skewed;
+        CG_REQUIRE(!overlap(a, na, p, n) && !overlap(b, nb, p, n) && (!w || !overlap(w, mats, p, n)));
     }
-    CG_REQUIRE(!overlap(ws, mats * sizeof(float), diags, out));
+    CG_REQUIRE(!overlap(ws, skewed, diags, out));
     const uint32_t row_blocks = (d1 + 63) / 64;
     float *m = static_cast<float *>(ws);
     CG_TRY(launch(low_rank_kernel, dim3(units * row_blocks, (d2 + 63) / 64), 256, 0, stream, w, a, b, m, (int)a_group, (int)d1, (int)d2,
-                  (int)rank, (int)row_blocks, c->T));
-    return encode<true>(c, stream, LdDiagonal<float>{m, c->logn, log_tile, log_diag, log_d2, (int)d1}, diags, units * n_diag);
+                  (int)rank, (int)row_blocks, (int)tile, c->T));
+    return encode<true>(c, stream, LdSkewed{D, m}, diags, units * n_diag);
 }
 
 CG_API size_t cg_cpvm_requests_workspace_bytes(const cg_req *c, uint32_t requests, uint32_t units, uint32_t n_diag)
@@ -333,16 +369,32 @@ static int cpvm_requests(cg_req *c, void *stream, const uint64_t *x, const void 
         for (uint32_t i = 1; i < n_diag; i++) gs[i - 1] = e = e * 3 % (2u * (uint32_t)c->N);
         CG_TRY(cg_rotate_hoisted(c->ctx, stream, x, n_diag - 1, gs, gk_copies, copies, requests, rest));
     }
-    CG_TRY(CG_ROWS(c, (size_t)requests * n_diag * 2 * c->k, stream, copies_kernel, , x, copies, f, (int)n_diag, c->T));
-    CG_TRY(CG_ROWS(c, (size_t)batch * 2 * c->k, stream, project_kernel, , f, static_cast<const double *>(diags),
-                   static_cast<const double *>(adapters), (int)n_adapters, pick, (int)units, (int)n_diag, xa, c->T));
-    uint64_t *cur = xa, *next = xb;
-    for (size_t r = 0, first = 0; r < counts.size(); first += counts[r], r++) {
-        uint64_t *to = r + 1 == counts.size() ? out : next;
-        if (round_bits) CG_TRY(cg_rotate_sum_hoisted(c->ctx, stream, cur, counts[r], elts.data() + first, gk_block + first, to, batch, rest));
-        else CG_TRY(cg_rotate(c->ctx, stream, cur, elts[first], gk_block[first], to, batch, 1, rest));
-        next = cur;
-        cur = to;
+    CG_TRY(CG_ROWS(c, (size_t)requests * n_diag * 2 * c->k, stream, (x, copies, f, (int)n_diag, c->T), copies_kernel));
+    const uint32_t blocks = (uint32_t)(c->N / (2 * PRODUCT_THREADS)) * c->k * requests;
+    // three workgroups to a compute unit are resident (one to twelve are within 1 %)
+    const uint32_t parts0 = std::min(units, std::max(1u, 3 * (uint32_t)c->n_cu / blocks)), per = (units + parts0 - 1) / parts0;
+    const ProductArgs A{f, static_cast<const double *>(diags), static_cast<const double *>(adapters), pick, reinterpret_cast<double *>(xa),
+                        (int)n_adapters, (int)requests, (int)units, (int)n_diag, (int)per, (int)((units + per - 1) / per)};
+    const unsigned grid = blocks * (unsigned)A.parts;
+    switch (n_diag) {
+    case 1: CG_TRY(launch(products_kernel<1, true>, dim3(grid), PRODUCT_THREADS, 0, stream, A, c->T)); break;
+    case 2: CG_TRY(launch(products_kernel<2, true>, dim3(grid), PRODUCT_THREADS, 0, stream, A, c->T)); break;
+    case 4: CG_TRY(launch(products_kernel<4, true>, dim3(grid), PRODUCT_THREADS, 0, stream, A, c->T)); break;
+    case 8: CG_TRY(launch(products_kernel<8, true>, dim3(grid), PRODUCT_THREADS, 0, stream, A, c->T)); break;
+    default: CG_TRY(launch(products_kernel<8, false>, dim3(grid), PRODUCT_THREADS, 0, stream, A, c->T));
+    }
+    CG_TRY(CG_ROWS(c, (size_t)batch * 2 * c->k, stream, (reinterpret_cast<double *>(xa), c->T), sums_kernel));
+    const size_t words = ct / 8;
+    for (uint32_t at_unit = 0, n; at_unit < batch; at_unit += n) {
+        n = round_bits ? fold_together(c, batch - at_unit) : batch;
+        uint64_t *cur = xa + at_unit * words, *next = xb + at_unit * words;
+        for (size_t r = 0, first = 0; r < counts.size(); first += counts[r], r++) {
+            uint64_t *to = r + 1 == counts.size() ? out + at_unit * words : next;
+            if (round_bits) CG_TRY(cg_rotate_sum_hoisted(c->ctx, stream, cur, counts[r], elts.data() + first, gk_block + first, to, n, rest));
+            else CG_TRY(cg_rotate(c->ctx, stream, cur, elts[first], gk_block[first], to, n, 1, rest));
+            next = cur;
+            cur = to;
+        }
     }
     return CG_OK;
 }
@@ -377,9 +429,18 @@ static int add_bias(cg_req *c, void *stream, const uint64_t *in, uint32_t groups
     CG_REQUIRE(in_one_call((uint64_t)groups * heads) && in_one_call((uint64_t)groups * heads * n_cts));
     const uint32_t units = groups * heads * n_cts;
     CG_REQUIRE(in == out || !overlap(in, ct_bytes(c) * units, out, ct_bytes(c) * units));
-    const int parts = 4;
-    const BiasArgs A{in, out, pos, table, edges, (int)n_buckets, (int)heads, (int)n_cts, log2_of(d2), parts};
-    return launch(bias_kernel, dim3(units * parts), BIAS_THREADS, (size_t)c->N / d2 * sizeof(float), stream, A, c->T);
+    const BiasArgs A{in, out, pos, table, edges, (int)n_buckets, (int)heads, (int)n_cts, log2_of(d2)};
+    const size_t lds = (size_t)c->N / d2 * sizeof(float);
+#define CG_BIAS(K) launch(bias_kernel<K, 2>, dim3(units * (unsigned)(c->N / (4 * BIAS_THREADS))), BIAS_THREADS, lds, stream, A, c->T)
+    switch (c->k) {
+    case 1: return CG_BIAS(1);
+    case 2: return CG_BIAS(2);
+    case 3: return CG_BIAS(3);
+    case 4: return CG_BIAS(4);
+    case 5: return CG_BIAS(5);
+    default: return CG_BIAS(6);
+    }
+#undef CG_BIAS
 }
 
 CG_API int cg_score_bias(cg_req *c, void *stream, const uint64_t *scores, uint32_t requests, uint32_t heads, uint32_t n_cts, uint32_t d2,
@@ -409,5 +470,7 @@ CG_API int cg_kv_append_requests(cg_req *c, void *stream, uint64_t *cache, uint3
     CG_REQUIRE(!overlap(cache, caches * cache_stride_cts * ct_bytes(c), rows, n_rows));
     const AppendArgs A{cache, rows, static_cast<const double *>(masks), lens, (int)per, log2_of((uint32_t)c->N / d2), cache_stride_cts,
                        row_stride_cts};
-    return CG_ROWS(c, caches * 2 * c->k, stream, append_kernel, , A, c->T);
+    // us, N = 8192, rows on 1024 threads / on 512: 144 rows 15.4 / 16.3, 576 43.2 / 40.7, 4608 244 / 237
+    const size_t all = caches * 2 * c->k;
+    return all > (size_t)c->n_cu ? CG_ROWS_WIDE(c, all, stream, (A, c->T), append_kernel) : CG_ROWS(c, all, stream, (A, c->T), append_kernel);
 }

