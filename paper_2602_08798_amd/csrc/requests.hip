@@ -102,16 +102,12 @@ int launch(void (*kernel)(P...), dim3 grid, unsigned block, size_t lds, void *s,
     return hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3(block), ptrs, lds, static_cast<hipStream_t>(s)) == hipSuccess
                ? CG_OK : CG_EHIP;
 }
-// KERNEL<LOGN, E, more> of ARGS for the handle's ring, a row to a workgroup.  WIDE: N = 8192 on 512 threads, two workgroups to a
-// compute unit
+// KERNEL<LOGN, E, more> of ARGS for the handle's ring, a row to a workgroup
 #define CG_LIST(...) __VA_ARGS__
-#define CG_ROWS_OF(c, rows, s, WIDE, ARGS, KERNEL, ...)                                                                                     \
-    ((c)->logn == 12 ? launch(KERNEL<12, 8 __VA_OPT__(, ) __VA_ARGS__>, dim3((unsigned)(rows)), 512, 0, s, CG_LIST ARGS)                   \
-     : (c)->logn == 14 ? launch(KERNEL<14, 16 __VA_OPT__(, ) __VA_ARGS__>, dim3((unsigned)(rows)), 1024, 0, s, CG_LIST ARGS)               \
-                       : launch(KERNEL<13, WIDE ? 16 : 8 __VA_OPT__(, ) __VA_ARGS__>, dim3((unsigned)(rows)), WIDE ? 512 : 1024, 0, s,     \
-                                CG_LIST ARGS))
-#define CG_ROWS(c, rows, s, ...) CG_ROWS_OF(c, rows, s, false, __VA_ARGS__)
-#define CG_ROWS_WIDE(c, rows, s, ...) CG_ROWS_OF(c, rows, s, true, __VA_ARGS__)
+#define CG_ROWS(c, rows, s, ARGS, KERNEL, ...)                                                                                        \
+    ((c)->logn == 12 ? launch(KERNEL<12, 8 __VA_OPT__(, ) __VA_ARGS__>, dim3((unsigned)(rows)), 512, 0, s, CG_LIST ARGS)              \
+     : (c)->logn == 13 ? launch(KERNEL<13, 8 __VA_OPT__(, ) __VA_ARGS__>, dim3((unsigned)(rows)), 1024, 0, s, CG_LIST ARGS)           \
+                       : launch(KERNEL<14, 16 __VA_OPT__(, ) __VA_ARGS__>, dim3((unsigned)(rows)), 1024, 0, s, CG_LIST ARGS))
 
 int create(cg_req *c, const cg_params *prm)
 {
@@ -192,8 +188,6 @@ int encode(const cg_req *c, void *s, LD ld, void *out, uint32_t batch)
         whole -= rest;
     }
     const int grid = whole + ((int)batch - whole) * split;
-    if constexpr (PREPARED)
-        if ((int)batch > cu) return CG_ROWS_WIDE(c, grid, s, (ld, out, c->T, whole, split), encode_kernel, PREPARED, LD);
     return CG_ROWS(c, grid, s, (ld, out, c->T, whole, split), encode_kernel, PREPARED, LD);
 }
 
@@ -470,7 +464,5 @@ CG_API int cg_kv_append_requests(cg_req *c, void *stream, uint64_t *cache, uint3
     CG_REQUIRE(!overlap(cache, caches * cache_stride_cts * ct_bytes(c), rows, n_rows));
     const AppendArgs A{cache, rows, static_cast<const double *>(masks), lens, (int)per, log2_of((uint32_t)c->N / d2), cache_stride_cts,
                        row_stride_cts};
-    // us, N = 8192, rows on 1024 threads / on 512: 144 rows 15.4 / 16.3, 576 43.2 / 40.7, 4608 244 / 237
-    const size_t all = caches * 2 * c->k;
-    return all > (size_t)c->n_cu ? CG_ROWS_WIDE(c, all, stream, (A, c->T), append_kernel) : CG_ROWS(c, all, stream, (A, c->T), append_kernel);
+    return CG_ROWS(c, caches * 2 * c->k, stream, (A, c->T), append_kernel);
 }

@@ -17,27 +17,90 @@ struct Tables {
     int logn, k;
 };
 
-// inv_row for a row whose elements lie in LDS already, behind a barrier
-template <int LOGN, int E, class ST>
-__device__ __forceinline__ void inv_row_placed(double *lds, const ST &st, int tid, const double *__restrict__ itw, const ModD m, int pr, const DevConst *C)
+// workgroups of 1024 threads with rows of 8192 in at most 64 registers a thread: two of them on a compute unit
+template <int LOGN, int E> constexpr int two_waves() { return LOGN == 13 && E == 8 ? 8 : min_waves<LOGN, E>(); }
+
+// A pass of the inverse transform modulo t < 2^20.  Centred inputs are below 2^19; after s stages without a reduction a sum is below
+// 2^(19 + s), its difference times a factor below 2^(39 + s) <= 2^52: every product is exact in one multiplication, and no sum is reduced (six
+// instructions a butterfly, where one modulo a 50-bit prime has eight and its passes reduce).  Plan and places as inv_pass.
+template <int LOGN, int E, int PASS>
+__device__ __forceinline__ void small_pass(double *lds, double *out, int tid, const double *__restrict__ itw, const double *twr, double *twr_next,
+                                           const ModD m, double ninv, double itw1_ninv)
+{
+    using P = Plan<LOGN, E>;
+    constexpr int R = P::R[PASS], L = LOGN - stage_start<LOGN, E, PASS>() - R, G = E >> R, PER = (1 << R) - 1;
+    constexpr bool last = PASS == 0;
+    static_assert(!last || G == 1, "one group a thread in the last pass");
+    auto times = [&](double x, double w) {
+        const double h = x * w;
+        return __builtin_fma(-__builtin_rint(h * m.u), m.p, h);
+    };
+    double v[G][1 << R];
+    int base[G];
+#pragma unroll
+    for (int g = 0; g < G; g++) {
+        const int at = group_index<LOGN, E, PASS>(tid, g);
+        base[g] = pad(((last ? 0 : at >> L) << (L + R)) | (at & ((1 << L) - 1)));
+#pragma unroll
+        for (int c = 0; c < (1 << R); c++) {
+            if (L > 0) v[g][c] = lds[base[g] + pad(c << L)];
+            else if (c % 2 == 0) {
+                const double2 x = pair_at(lds, base[g] + c);
+                v[g][c] = x.x;
+                v[g][c + 1] = x.y;
+            }
+        }
+    }
+#pragma unroll
+    for (int g = 0; g < G; g++)
+#pragma unroll
+        for (int u = R - 1; u >= 0; u--) {
+            const int half = 1 << (R - 1 - u);
+#pragma unroll
+            for (int c = 0; c < (1 << R); c++) {
+                if (c & half) continue;
+                const double sum = v[g][c] + v[g][c + half], d = v[g][c] - v[g][c + half];
+                v[g][c] = last && u == 0 ? times(sum, ninv) : sum;
+                v[g][c + half] = times(d, last && u == 0 ? itw1_ninv : twr[g * PER + (1 << u) - 1 + (c >> (R - u))]);
+            }
+        }
+    if constexpr (last) {
+#pragma unroll
+        for (int c = 0; c < (1 << R); c++) out[c] = v[0][c];        // (element tid + c * T)
+    } else {
+        if constexpr (PASS == 1) load_tw<LOGN, E, 0, true>(itw, tid, twr_next);
+        else load_tw<LOGN, E, PASS - 1, false>(itw, tid, twr_next);
+#pragma unroll
+        for (int g = 0; g < G; g++)
+#pragma unroll
+            for (int c = 0; c < (1 << R); c++) {
+                if (L > 0) lds[base[g] + pad(c << L)] = v[g][c];
+                else if (c % 2 == 0) pair_at(lds, base[g] + c) = make_double2(v[g][c], v[g][c + 1]);
+            }
+        if constexpr (PASS - 1 < P::NC) lds_barrier();
+        else wave_sync();
+    }
+}
+// The row lies in LDS, behind a barrier; results |x| <= (1/2 + 2^-18) t, element tid + c * T in out[c]
+template <int LOGN, int E>
+__device__ __forceinline__ void small_inv_row(double *lds, double *out, int tid, const double *__restrict__ itw, const ModD m, double ninv, double itw1_ninv)
 {
     constexpr int NP = Plan<LOGN, E>::NP;
     asm volatile("" : "+v"(tid));
-    double twa[TWREGS], twb[TWREGS], in[E];
+    double twa[TWREGS], twb[TWREGS];
     load_tw<LOGN, E, NP - 1, false>(itw, tid, twa);
-    if constexpr (Plan<LOGN, E>::R[NP - 1] == 1) {
-#pragma unroll
-        for (int it = 0; it < E; it += 2) {
-            const double2 x = pair_at(lds, pad(chunk_elem<E>(tid, it)));
-            in[it] = x.x;
-            in[it + 1] = x.y;
-        }
+    if constexpr (NP > 4) {
+        small_pass<LOGN, E, 4>(lds, out, tid, itw, twa, twb, m, ninv, itw1_ninv);
+        small_pass<LOGN, E, 3>(lds, out, tid, itw, twb, twa, m, ninv, itw1_ninv);
+        small_pass<LOGN, E, 2>(lds, out, tid, itw, twa, twb, m, ninv, itw1_ninv);
+        small_pass<LOGN, E, 1>(lds, out, tid, itw, twb, twa, m, ninv, itw1_ninv);
+        small_pass<LOGN, E, 0>(lds, out, tid, itw, twa, twb, m, ninv, itw1_ninv);
+    } else {
+        small_pass<LOGN, E, 3>(lds, out, tid, itw, twa, twb, m, ninv, itw1_ninv);
+        small_pass<LOGN, E, 2>(lds, out, tid, itw, twb, twa, m, ninv, itw1_ninv);
+        small_pass<LOGN, E, 1>(lds, out, tid, itw, twa, twb, m, ninv, itw1_ninv);
+        small_pass<LOGN, E, 0>(lds, out, tid, itw, twb, twa, m, ninv, itw1_ninv);
     }
-    inv_pass<LOGN, E, NP - 1>(lds, st, 0, tid, itw, twa, twb, m, pr, C, in);
-    if constexpr (NP > 4) inv_pass<LOGN, E, 3>(lds, st, 0, tid, itw, twb, twa, m, pr, C);
-    inv_pass<LOGN, E, 2>(lds, st, 0, tid, itw, NP > 4 ? twa : twb, NP > 4 ? twb : twa, m, pr, C);
-    inv_pass<LOGN, E, 1>(lds, st, 0, tid, itw, NP > 4 ? twb : twa, NP > 4 ? twa : twb, m, pr, C);
-    inv_pass<LOGN, E, 0>(lds, st, 0, tid, itw, NP > 4 ? twa : twb, NP > 4 ? twb : twa, m, pr, C);
 }
 
 // ---------------------------------------------------------------------------
@@ -81,7 +144,7 @@ struct LdSkewed : Diagonal {        // float [units][tile][d2], row (f - col) mo
 
 // The first `whole` plaintexts take a workgroup each, those behind `split`, which share the primes and repeat the interpolation.
 template <int LOGN, int E, bool PREPARED, class LD>
-__global__ void __launch_bounds__((1 << LOGN) / E, (min_waves<LOGN, E>()))
+__global__ void __launch_bounds__((1 << LOGN) / E, (two_waves<LOGN, E>()))
 encode_kernel(LD ld, void *__restrict__ out, Tables T, int whole, int split)
 {
     __shared__ __align__(16) double lds[lds_doubles<LOGN>()];
@@ -95,7 +158,7 @@ encode_kernel(LD ld, void *__restrict__ out, Tables T, int whole, int split)
 #pragma unroll
     for (int it = 0; it < E; it++) lds[pad((int)at_lane(T.place + it * TH, tid))] = red(v[it], mt);
     lds_barrier();
-    inv_row_placed<LOGN, E>(lds, StRegs{w}, tid, T.itw + ((size_t)k << LOGN), mt, k, T.C);
+    small_inv_row<LOGN, E>(lds, w, tid, T.itw + ((size_t)k << LOGN), mt, T.C->ninv[k], T.C->itw1_ninv[k]);
     if constexpr (!PREPARED) {
         uint64_t *row = static_cast<uint64_t *>(out) + ((size_t)b << LOGN);
 #pragma unroll
@@ -408,7 +471,7 @@ struct AppendArgs {
     uint32_t stride, row_stride;
 };
 template <int LOGN, int E>
-__global__ void __launch_bounds__((1 << LOGN) / E, (min_waves<LOGN, E>()))
+__global__ void __launch_bounds__((1 << LOGN) / E, (two_waves<LOGN, E>()))
 append_kernel(AppendArgs A, Tables T)
 {
     __shared__ __align__(16) double lds[lds_doubles<LOGN>()];
