@@ -49,7 +49,7 @@ int cg_slots_prepare(cg_req *req, void *stream, const int64_t *slots_dev, void *
  * at cg_cpvm: tiles of D1 = the power of two >= max(d1, d2, N/d2), at most N/2; n_diag = d2 D1 / N,
  * at most 64.  d2 a power of two, 2 <= d2 <= N/4; rank <= 4096.  diags_dev: prepared plaintexts
  * [units][n_diag].  units n_diag <= 65536.
- * ws_dev: cg_cpvm_prepare_workspace_bytes(...) bytes (0 with rank = 0: ws_dev may then be NULL). */
+ * ws_dev: cg_cpvm_prepare_workspace_bytes(...) bytes (where that is 0 ws_dev may be NULL). */
 uint32_t cg_cpvm_diagonals(const cg_req *req, uint32_t d1, uint32_t d2);    /* n_diag; 0: sizes out of range */
 size_t cg_cpvm_prepare_workspace_bytes(const cg_req *req, uint32_t units, uint32_t d1, uint32_t d2, uint32_t rank);
 int cg_cpvm_prepare(cg_req *req, void *stream, const int64_t *w_dev, const int64_t *a_dev, const int64_t *b_dev,

@@ -187,40 +187,77 @@ encode_kernel(LD ld, void *__restrict__ out, Tables T, int whole, int split)
 }
 
 // ---------------------------------------------------------------------------
-// M_u = W_u + A B_u modulo t for the diagonals of adapters: 16 x 16 tiles on the matrix cores in FP64, exact because centred
-// entries are below 2^19 and rank 2^38 below 2^53.  A wave takes 16 features and up to 64 columns.
+// M_u = W_u + A B_u modulo t, laid out by its diagonals: 64 x 64 entries to a workgroup on the matrix cores in FP64, exact because centred
+// entries are below 2^19 and rank 2^38 below 2^53.  Bound by its loads and stores, which for a rank of 16 are a hundredth of the encoded
+// diagonals': factors are brought in and centred once a workgroup, and the tile leaves through LDS, a diagonal's entries side by
+// side (each lane's own entry to its own row took 16.8 us for 36 matrices of 768 x 64 at rank 16, and 34.4 at 64).
 // ---------------------------------------------------------------------------
 typedef double cg_double4v __attribute__((ext_vector_type(4)));
+constexpr int LR_TILE = 64, LR_RANK = 16;
 __global__ void __launch_bounds__(256)
 low_rank_kernel(const int64_t *__restrict__ w, const int64_t *__restrict__ a, const int64_t *__restrict__ b, float *__restrict__ out, int a_group,
-                int d1, int d2, int rank, int row_blocks, int tile, Tables T)
+                int d1, int log_d2, int rank, int row_blocks, int tile, Tables T)
 {
+    __shared__ double as[LR_TILE][LR_RANK + 1], bs[LR_RANK][LR_TILE + 2];
+    __shared__ float done[LR_TILE][LR_TILE + 1];
     const ModD mt = T.C->mod[T.k];
-    const int u = (int)blockIdx.x / row_blocks, lane = threadIdx.x & 63;
-    const int f0 = ((int)blockIdx.x % row_blocks) * 64 + ((int)threadIdx.x >> 6) * 16, c0 = (int)blockIdx.y * 64;
+    const int d2 = 1 << log_d2, u = (int)blockIdx.x / row_blocks, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int f0 = ((int)blockIdx.x % row_blocks) * LR_TILE, c0 = (int)blockIdx.y * LR_TILE;
     const int i = lane & 15, q = lane >> 4;
     const int64_t *au = a + (size_t)(u / a_group) * d1 * rank, *bu = b + (size_t)u * rank * d2;
     cg_double4v acc[4] = {};
-    for (int j0 = 0; j0 < rank; j0 += 4) {
-        const int j = j0 + q;
-        const double x = f0 + i < d1 && j < rank ? red((double)(int)au[(size_t)(f0 + i) * rank + j], mt) : 0.0;
+    // (W's words come in beside the products)
+    const int64_t *wu = w + (((size_t)u * d1) << log_d2);
+    int base[4][4];
 #pragma unroll
-        for (int c = 0; c < 4; c++) {
-            const int col = c0 + 16 * c + i;
-            const double y = col < d2 && j < rank ? red((double)(int)bu[(size_t)j * d2 + col], mt) : 0.0;
-            acc[c] = __builtin_amdgcn_mfma_f64_16x16x4f64(x, y, acc[c], 0, 0, 0);
+    for (int c = 0; c < 4; c++)
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            const int f = f0 + 16 * wave + 4 * e + q, col = c0 + 16 * c + i;
+            base[c][e] = w && f < d1 && col < d2 ? (int)at32(wu, (f << log_d2) + col) : 0;
+        }
+    for (int j0 = 0; j0 < rank; j0 += LR_RANK) {
+        int64_t x[4], y[4];
+        const int af = f0 + (tid >> 2), aj = j0 + 4 * (tid & 3), bj = j0 + (tid >> 4), bc = c0 + 4 * (tid & 15);
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            x[e] = af < d1 && aj + e < rank ? au[(size_t)af * rank + aj + e] : 0;
+            y[e] = bj < rank && bc + e < d2 ? bu[(size_t)bj * d2 + bc + e] : 0;
+        }
+        if (j0) __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 4; e++) {
+            as[tid >> 2][4 * (tid & 3) + e] = red((double)(int)x[e], mt);
+            bs[tid >> 4][4 * (tid & 15) + e] = red((double)(int)y[e], mt);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < LR_RANK; n += 4) {
+            if (j0 + n >= rank) break;
+            const double xn = as[16 * wave + i][n + q];
+#pragma unroll
+            for (int c = 0; c < 4; c++) acc[c] = __builtin_amdgcn_mfma_f64_16x16x4f64(xn, bs[n + q][16 * c + i], acc[c], 0, 0, 0);
         }
     }
 #pragma unroll
     for (int c = 0; c < 4; c++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) {
-            const int f = f0 + 4 * e + q, col = c0 + 16 * c + i;
-            if (f >= d1 || col >= d2) continue;
-            double v = red(acc[c][e], mt);
-            if (w) v = red(v + (double)(int)w[((size_t)u * d1 + f) * d2 + col], mt);
-            out[((size_t)u * tile + ((f - col) & (tile - 1))) * d2 + col] = (float)v;
+        for (int e = 0; e < 4; e++) done[16 * wave + 4 * e + q][16 * c + i] = (float)red(red(acc[c][e], mt) + (double)base[c][e], mt);
+    __syncthreads();
+    // feature - column = dd - 63 within the tile: a row of the layout to a wave at a time
+    float *mine = out + (((size_t)u * tile) << log_d2);
+    const bool there = c0 + lane < d2;
+#pragma unroll
+    for (int d0 = 0; d0 < 2 * LR_TILE; d0 += 32) {
+        float v[8];
+#pragma unroll
+        for (int n = 0; n < 8; n++) v[n] = done[(d0 + 4 * n + wave - (LR_TILE - 1) + lane) & (LR_TILE - 1)][lane];
+#pragma unroll
+        for (int n = 0; n < 8; n++) {
+            const int f = d0 + 4 * n + wave - (LR_TILE - 1) + lane;
+            if (there && f >= 0 && f < LR_TILE && f0 + f < d1) put32(mine, (((f0 + f - c0 - lane) & (tile - 1)) << log_d2) + c0 + lane, v[n]);
         }
+    }
 }
 
 // ---------------------------------------------------------------------------

@@ -110,7 +110,8 @@ class Requests:
         rows = self._rows(int(units) * self.cpvm_diagonals(d1, d2) * self.k)
         out = self._empty(rows, torch.float64) if out is None else out
         _need(out, rows, "out (prepared)")
-        ws = self._workspace(int(self.lib.dll.cg_cpvm_prepare_workspace_bytes(self.h, units, d1, d2, rank))) if rank else None
+        need = int(self.lib.dll.cg_cpvm_prepare_workspace_bytes(self.h, units, d1, d2, rank))
+        ws = self._workspace(need) if need else None
         self._call("cg_cpvm_prepare", _ints(w, torch.int64, int(units) * int(d1) * int(d2), "w"), _ints(a, torch.int64, 0, "a"),
                    _ints(b, torch.int64, 0, "b"), units, a_group, d1, d2, rank, _ptr(out), _ptr(ws))
         return out

@@ -127,7 +127,7 @@ def _unreached(lib):
                 b = u32(n)
                 go("cg_slots_encode", d, far, b)
                 go("cg_slots_prepare", d, far, b)
-                go("cg_cpvm_prepare", d, None, None, b, u32(1), u32(100), u32(64), u32(0), far, None)
+                go("cg_cpvm_prepare", d, None, None, b, u32(1), u32(100), u32(64), u32(0), far, farther)
                 go("cg_cpvm_prepare", None, d, d, b, u32(1), u32(100), u32(64), u32(8), far, farther)
                 for d1, n_diag in ((100, f.cg_cpvm_diagonals(h, u32(100), u32(64))), (2048, f.cg_cpvm_diagonals(h, u32(2048), u32(64)))):
                     go("cg_cpvm_requests", d, d, d, u32(2), at4, b, u32(1), u32(n_diag), u32(64), u32(3), KEYS, KEYS, far, farther)
