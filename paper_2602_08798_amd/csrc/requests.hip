@@ -191,20 +191,24 @@ int encode(const cg_req *c, void *s, LD ld, void *out, uint32_t batch)
     return CG_ROWS(c, grid, s, (ld, out, c->T, whole, split), encode_kernel, PREPARED, LD);
 }
 
-// How many of the ciphertexts that are left go through their rounds together, at N = 8192: whole rounds of the compute units first.  The evaluator
-// takes a unit's key switch on one workgroup where the last round of units is nine tenths full, and the (unit, prime) rows where theirs
-// is nearly full; with a few units more than that, every launch of the whole call is of the slower kind.  us a round of 7 / 3
-// rotations, in one call and with whole rounds first: 576 units 703 / 558 and 594 / 473, 540 680 / 544 and 570 / 461, 700 852 / 585 and 745 / 596,
-// 320 399 / 318 and 377 / 266, 288 377 / 302 and 361 / 259, 144 224 / 181 and 185 / 144, 72 120 / 98 and 113 / 92; beyond the limits 200 265 / 210
-// and 260 / 207, 108 130 / 102 and 153 / 117.  (N = 4096: 576 units 187 / 151 and 179 / 138, 300 106 / 84 and 111 / 91; N = 16384: 40 292 / 239 and 275 / 230,
-// 96 and more even: left whole.)
+// How many of the ciphertexts that are left go through their rounds together: whole rounds of the compute units first.  The evaluator takes a
+// unit's key switch on one workgroup, or its (unit, prime) rows on one each, where these nearly fill their last round; with a few units
+// more, every launch of the call is of the slower kind.  us a projection of one diagonal in one call / whole rounds first, one special prime (a round: as
+// many units as have a compute unit for every row).
+// - N = 8192.  A round and up to a quarter: k = 3 72 units 351 / 330, k = 2 95 287 / 280, k = 4 57 497 / 392, k = 6 40 533 / 517 (and a half: 96 431 / 424, 127 344 / 348, 76
+//   464 / 511, 54 599 / 675).  Two and up to a half: k = 3 144 626 / 535, k = 2 191 489 / 455, k = 4 114 900 / 613, k = 6 81 1038 / 812 (three: 192 670 / 670, 255 523 /
+//   541).  Units' own rounds, from two on: k = 3 576 1972 / 1754, k = 1 608 / 563, k = 2 1212 / 1117, k = 4 2796 / 2779, k = 6 5114 / 4631; from one with three
+//   digits only: k = 3 288 1091 / 1014, 384 1284 / 1241, but k = 2 288 616 / 641, k = 4 1445 / 1519.
+// - N = 4096, units' own rounds from two on: k = 2 520 433 / 428, 600 500 / 489, 800 633 / 580, k = 4 600 1166 / 1137 (640 515 / 517; 300 264 / 263).
+// - N = 16384, rounds and up to a quarter: k = 6, two special primes, 36 854 / 743, k = 3 72 814 / 679, k = 6 40 1226 / 1021 (and a half: 96 928 / 939, 54 1474 / 1510).
+// (N = 8192 with two special primes has no such kernels: 36 398 / 429, 288 2643 / 2705.)
 uint32_t fold_together(const cg_req *c, uint32_t left)
 {
-    const uint32_t cu = (uint32_t)c->n_cu, rest = left % cu;
-    if (c->logn != 13) return left;
-    if (left >= cu) return 10 * rest >= 9 * cu ? left : left - rest;
-    if (2 * left > cu && 8 * left <= 5 * cu) return cu / 2;
-    if (4 * left > cu && 5 * left <= 2 * cu) return cu / 4;
+    const uint32_t cu = (uint32_t)c->n_cu, round = std::max(1u, cu / (uint32_t)(c->k + c->nsp)), rest = left % cu, over = left % round;
+    if (c->logn == 14) return left > round && 4 * over <= round ? left - over : left;
+    if (c->nsp > 1) return left;
+    if (left >= 2 * cu || (c->logn == 13 && c->k == 3 && left >= cu)) return (c->logn == 13 ? 10 * rest < 9 * cu : 5 * rest <= 2 * cu) ? left - rest : left;
+    if (c->logn == 13 && left < cu && left > round && left < 3 * round && (left < 2 * round ? 4 : 2) * over <= round) return left - over;
     return left;
 }
 

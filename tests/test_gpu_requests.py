@@ -68,6 +68,68 @@ def test_slots_are_encoded_as_the_codec_does(name, batch):
     assert torch.equal(plain, ref)
 
 
+@pytest.mark.parametrize("log2n,t", [(12, 40961), (12, 1032193), (13, 1032193), (14, 786433)])
+def test_other_plaintext_moduli(log2n, t):
+    """Small ones and the largest below 2^20, where exact products and centred values are at their bounds."""
+    import paper_2602_08798_amd as P
+    from tests.bruteforce import ntt_primes
+    from workloads.params import ParamSet
+    k = {12: 2, 13: 1, 14: 2}[log2n]
+    p = ntt_primes(1 << 50, 2 << log2n, k + 1)
+    prm = ParamSet("x", log2n, q=tuple(p[:k]), p=tuple(p[k:]), t=t)
+    ctx, codec, n = P.Context(prm), SlotCodec(prm), prm.n
+    rq = P.Requests(ctx)
+    say(f"t = {t}, N = {n}")
+    v = _slots(n, 9, t, t)
+    got = P.to_host(rq.slots_encode(_ints(v)))
+    for i in range(9):
+        assert np.array_equal(got[i], codec.encode(v[i])), i
+    import torch
+    assert torch.equal(rq.slots_prepare(_ints(v)), ctx.plain_prepare(P.to_device(got)))
+    # an adapter of the largest rank with entries of the largest size
+    h = (t - 1) // 2
+    a, b = np.full((1, 64, 4096), h), np.full((1, 4096, 64), -h)
+    b[0, :, 0], b[0, :, 1] = h, np.arange(4096) % 2 * 2 * h - h
+    M = np.zeros((64, 64), dtype=np.int64)
+    M[:] = [int(sum(h * int(x) for x in b[0, :, c])) % t for c in range(64)]
+    C = rq.cpvm_diagonals(64, 64)
+    want = np.stack([codec.encode(attention.cpvm_weight_values(n, 64, 64, M, c)) for c in range(C)])
+    assert torch.equal(rq.cpvm_prepare(1, 64, 64, a=_ints(a), b=_ints(b)), ctx.plain_prepare(P.to_device(want)))
+    table, edges = np.array([[h], [-h], [t - 1], [1]]), np.array([0, 1, 2, 9])
+    orc = __import__("oracle").Oracle(prm)
+    from workloads import pseudo_ciphertexts
+    x = pseudo_ciphertexts(Stream(5, 1), prm.q, n, 1)
+    out = P.to_host(rq.score_bias(P.to_device(x), 1, 1, 1, 64, _lens([n // 64 - 1]), _ints(table), _lens(edges)))
+    assert np.array_equal(out[0], orc.add_plain(x[0], codec.encode(attention.score_bias_values(n, 64, 0, n // 64 - 1, table, edges, 0))))
+
+
+def test_a_modulus_without_slots_has_no_handle():
+    import paper_2602_08798_amd as P
+    from paper_2602_08798_amd.binding import CgError
+    from dataclasses import replace
+    from workloads import PRESETS
+    ctx = P.Context(replace(PRESETS["C1"], t=65521))
+    with pytest.raises(CgError):
+        P.Requests(ctx)
+
+
+def test_a_closed_handle_or_context_is_refused():
+    import paper_2602_08798_amd as P
+    from paper_2602_08798_amd.binding import CgError
+    from workloads import PRESETS
+    ctx = P.Context(PRESETS["C1"])
+    first, second = P.Requests(ctx), P.Requests(ctx)
+    v = _ints(np.zeros((1, ctx.n)))
+    first.slots_encode(v)
+    first.close()
+    with pytest.raises(CgError):
+        first.slots_encode(v)
+    second.slots_encode(v)
+    ctx.close()
+    with pytest.raises(CgError):
+        second.slots_encode(v)
+
+
 def _matrices(rng, units, d1, d2, rank, a_group, base, lo=-128, hi=128):
     return (rng.integers(lo, hi, (units, d1, d2)) if base else None,
             rng.integers(lo, hi, (-(-units // a_group), d1, rank)) if rank else None,
