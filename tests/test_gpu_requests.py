@@ -216,6 +216,30 @@ def test_projections_without_adapters_are_those_of_one_request():
         assert torch.equal(got[r], env.ctx.cpvm_hoisted(x[r], diags, units, C, d2, copies, block, block_round_bits=3)), r
 
 
+@pytest.mark.parametrize("name,requests,units,d1,bits", [("C2", 9, 8, 64, 3), ("C2", 12, 12, 64, 3), ("C2", 8, 36, 64, 4), ("C2", 1, 576, 64, 3),
+                                                        ("C1", 13, 41, 64, 3), ("C5", 9, 4, 64, 3), ("C2", 17, 1, 768, 0)])
+def test_large_calls_are_the_small_ones(name, requests, units, d1, bits):
+    """Calls whose rounds are cut into whole rounds of the compute units and the rest, with adapters: each request against the call
+    for one request with its adapter's diagonals added to the base's."""
+    import torch
+    env = _env(name)
+    d2, q = 64, torch.tensor(env.prm.q, dtype=torch.float64, device="cuda")[:, None]
+    C = attention.cpvm_shape(env.n, d1, d2)[2]
+    say(f"cpvm_requests {name}: {requests} x {units}, {C} diagonals, {bits} bits")
+    copies, block, _ = _projection(env, d1, d2, bits, 500)
+    rng = np.random.default_rng(units)
+    base = env.rq.cpvm_prepare(units, d1, d2, w=_ints(rng.integers(-128, 128, (units, d1, d2))))
+    low = torch.stack([env.rq.cpvm_prepare(units, d1, d2, a=_ints(rng.integers(-128, 128, (1, d1, 3))), b=_ints(rng.integers(-128, 128, (units, 3, d2))),
+                                           a_group=units) for _ in range(2)])
+    x = env.dev(env.cts(7, requests))
+    pick = [(0, 1, -1)[r % 3] for r in range(requests)]
+    got = env.rq.cpvm_requests(x, base, requests, units, C, d2, copies, block, adapters=low, pick=_lens(pick), block_round_bits=bits)
+    for r in range(requests):
+        both = base.view(-1, env.k, env.n) + (low[pick[r]].view(-1, env.k, env.n) if pick[r] >= 0 else 0)
+        both = torch.where(both > q / 2, both - q, torch.where(both < -q / 2, both + q, both)).contiguous()
+        assert torch.equal(got[r], env.ctx.cpvm_hoisted(x[r], both, units, C, d2, copies, block, block_round_bits=bits)), r
+
+
 def _bias_case(env, heads, buckets, seed, first=0):
     rng = np.random.default_rng(seed)
     edges = first + np.cumsum(np.concatenate([[0], rng.integers(1, 40, buckets - 1)]))
