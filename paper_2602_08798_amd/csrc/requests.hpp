@@ -297,6 +297,15 @@ struct ProductArgs {
     int n_adapters, requests, units, n_diag, per, parts;
 };
 constexpr int PRODUCT_THREADS = 256;
+// at_lane for what is read once: it leaves the caches to what is read again
+template <class T> __device__ __forceinline__ T at_lane_once(const T *base, int tid)
+{
+    auto g = (const T __attribute__((address_space(1))) *)base;
+    uint32_t off = (uint32_t)tid * (uint32_t)sizeof(T);
+    asm("" : "+s"(g));
+    asm("" : "+v"(off));
+    return __builtin_nontemporal_load((const T __attribute__((address_space(1))) *)((const char __attribute__((address_space(1))) *)g + off));
+}
 // C copies at a time; HELD: all there are
 template <int C, bool HELD, bool PLUS>
 __device__ __forceinline__ void products_of(const cg_double2v *x, const cg_double2v *w, const cg_double2v *plus, cg_double2v *out, int n_diag,
@@ -319,7 +328,7 @@ __device__ __forceinline__ void products_of(const cg_double2v *x, const cg_doubl
 #pragma unroll
             for (int c = 0; c < C; c++) {
                 b[c] = at_lane(w + (size_t)(c0 + c) * k * row, lane);
-                if constexpr (PLUS) e[c] = at_lane(plus + (size_t)(c0 + c) * k * row, lane);
+                if constexpr (PLUS) e[c] = at_lane_once(plus + (size_t)(c0 + c) * k * row, lane);
             }
             // four products of a centred factor and one twice as large, or eight of two centred ones: DotSum's room
             constexpr int ROOM = PLUS ? DotSum::CANONICAL : DotSum::CENTRED;
