@@ -107,7 +107,10 @@ __device__ __forceinline__ void small_inv_row(double *lds, double *out, int tid,
 // Slot values -> polynomial modulo t -> prepared plaintext.  The interpolation is an inverse transform modulo t of the
 // values in the order of the transform's outputs; its results are centred in registers and go through one forward
 // transform per ciphertext prime without leaving the workgroup.  Values are read in the order of the slots, which their
-// sources hold side by side, and put in their places in LDS.
+// sources hold side by side, and put in their places in LDS (read in the order of the places 300 plaintexts took 52.4 us, now 47.9).
+// Bound by vector issue: 1000 plaintexts of N = 8192 and three primes take 91 us, 22.8 ns a row transform, their 262 MB at the rate of a
+// copy would take 49; in 75 registers with one workgroup to a unit 102, with the interpolation by the passes for 50-bit primes 93.6.  One plaintext
+// takes 12.0 us with its primes on workgroups of their own, one after the other 22.5.
 // ---------------------------------------------------------------------------
 struct LdSlots {
     const int64_t *v;
@@ -261,7 +264,7 @@ low_rank_kernel(const int64_t *__restrict__ w, const int64_t *__restrict__ a, co
 }
 
 // ---------------------------------------------------------------------------
-// The copies of all tokens, transformed: row (r, c, component, prime), copy 0 being the token itself
+// The copies of all tokens, transformed: row (r, c, component, prime), copy 0 being the token itself.  768 rows of 8192 (16 requests) 24 us.
 // ---------------------------------------------------------------------------
 template <int LOGN, int E>
 __global__ void __launch_bounds__((1 << LOGN) / E, (min_waves<LOGN, E>()))
@@ -287,8 +290,10 @@ copies_kernel(const uint64_t *__restrict__ x, const uint64_t *__restrict__ copie
 // ---------------------------------------------------------------------------
 // y[r][u] = sum over c of copy_(r, c) times (diagonal_(u, c) + that of the request's adapter), transformed: a thread takes a pair of
 // coefficients of one request and prime through `per` units, both components, so that a diagonal's word is read once for both and
-// the copies' words (up to eight copies) stay in registers.  Bound by the diagonals' way from memory: an adapter's are read by its
-// request alone.
+// the copies' words (up to eight copies) stay in registers.  Bound by the diagonals' way from memory, as an adapter's are read by its
+// request alone: 16 requests with an adapter each, 36 matrices of 8 diagonals, N = 8192, 1.19 GB in 246 us (4.8 TB/s, a copy reaches 5.4).  As the
+// loader of the inverse transforms, a row to a workgroup, each component read the diagonals for itself and the pass took 692 us
+// (with four copies' words asked for together 430 to 466), here 246 and 89 for the transforms.
 // ---------------------------------------------------------------------------
 struct ProductArgs {
     const double *copies, *diags, *adapters;
@@ -376,7 +381,7 @@ products_kernel(ProductArgs A, Tables T)
     else
         products_of<C, HELD, false>(x, w, w, out, A.n_diag, n, k, logn, lane, m);
 }
-// rows of such sums back in coefficients, in place
+// Rows of such sums back in coefficients, in place: 3456 rows of 8192 in 89 us, 5.1 TB/s.
 template <int LOGN, int E>
 __global__ void __launch_bounds__((1 << LOGN) / E, (min_waves<LOGN, E>()))
 sums_kernel(double *rows, Tables T)
@@ -401,7 +406,9 @@ sums_kernel(double *rows, Tables T)
 // Position biases.  Only slots b d2 carry one: the values at zeta^(+-e), e = 3^(d2 b) = 1 modulo 4 d2, which are the
 // roots of X^n' - w and X^n' - 1/w with n' = N / (2 d2), w = zeta^n'.  So the polynomial is
 //   m_j = N^-1 (A_(j mod n') zeta^-j + B_(j mod n') zeta^j),  A, B transforms of n' points of the two rows' values,
-// two products a coefficient where the interpolation of any slots takes log2(N) / 2.
+// two products a coefficient where the interpolation of any slots takes log2(N) / 2.  Bound by component 0's way from memory and
+// back: 1536 ciphertexts of N = 8192 and three primes in 124 us, 4.9 TB/s; 384 in 31.5 (the words asked for behind the bias 34.9; a part of four times as many
+// coefficients, with as many loads in flight, 35.6).
 // ---------------------------------------------------------------------------
 struct BiasArgs {
     const uint64_t *in;
@@ -506,7 +513,9 @@ bias_kernel(BiasArgs A, Tables T)
 
 // ---------------------------------------------------------------------------
 // Append at each request's own length: row (request, cache, component, prime), its transform, the product with the block's mask and the
-// transform back in one workgroup.  A request whose length has no place leaves at once.
+// transform back in one workgroup.  A request whose length has no place leaves at once.  Bound by vector issue (75 % busy on 4032 rows of
+// 8192, 58 ns each; their bytes alone would take 36): 64 registers a thread, so that two workgroups of 1024 threads share a unit (234 us; rows on 512
+// threads 238, in 66 registers 243).  Mask and addends asked for with the row 266: loads return in order, and the passes' factors wait.
 // ---------------------------------------------------------------------------
 struct AppendArgs {
     uint64_t *cache;
