@@ -202,8 +202,13 @@ int encode(const cg_req *c, void *s, LD ld, void *out, uint32_t batch)
 // - N = 4096, units' own rounds from two on: k = 2 520 433 / 428, 600 500 / 489, 800 633 / 580, k = 4 600 1166 / 1137 (640 515 / 517; 300 264 / 263).
 // - N = 16384, rounds and up to a quarter: k = 6, two special primes, 36 854 / 743, k = 3 72 814 / 679, k = 6 40 1226 / 1021 (and a half: 96 928 / 939, 54 1474 / 1510).
 // (N = 8192 with two special primes has no such kernels: 36 398 / 429, 288 2643 / 2705.)
+//
+// At most so many units go together at all: the workspace is theirs (5 to 7 GB), and their kernels have long filled the chip.  us, 1 / 2 / 4 / 8 units to a
+// compute unit: N = 8192 2304 units 7316 / 6820 / 6809 / 6844, N = 4096 1764 / 1601 / 1575 / 1545, N = 16384 384 units 6717 / 6668 / 6658 / 6669.
+uint32_t most_together(const cg_req *c) { return (c->logn == 14 ? 1u : c->logn == 13 ? 4u : 8u) * (uint32_t)c->n_cu; }
 uint32_t fold_together(const cg_req *c, uint32_t left)
 {
+    if (left > most_together(c)) return most_together(c);
     const uint32_t cu = (uint32_t)c->n_cu, round = std::max(1u, cu / (uint32_t)(c->k + c->nsp)), rest = left % cu, over = left % round;
     if (c->logn == 14) return left > round && 4 * over <= round ? left - over : left;
     if (c->nsp > 1) return left;
@@ -332,12 +337,16 @@ CG_API int cg_cpvm_prepare(cg_req *c, void *stream, const int64_t *w, const int6
     return encode<true>(c, stream, LdSkewed{D, m}, diags, units * n_diag);
 }
 
+// requests whose copies are made together
+static uint32_t series_together(const cg_req *c, uint32_t requests, uint32_t n_diag) { return std::min(requests, std::max(1u, most_together(c) / n_diag)); }
+
 CG_API size_t cg_cpvm_requests_workspace_bytes(const cg_req *c, uint32_t requests, uint32_t units, uint32_t n_diag)
 {
     if (!c || !in_one_call((uint64_t)requests * units) || !n_diag || n_diag > 64 || !in_one_call((uint64_t)requests * n_diag)) return 0;
-    const size_t copies = n_diag - 1, cts = requests * copies + (size_t)requests * n_diag + 2 * (size_t)requests * units;
-    const size_t series = copies ? cg_workspace_bytes(c->ctx, (uint32_t)(requests * copies + requests)) : 0;
-    return cts * ct_bytes(c) + std::max(series, cg_workspace_bytes(c->ctx, requests * units));
+    const size_t copies = n_diag - 1, batch = (size_t)requests * units, together = std::min(batch, (size_t)most_together(c));
+    const size_t cts = requests * copies + (size_t)requests * n_diag + batch + together;
+    const size_t series = copies ? cg_workspace_bytes(c->ctx, series_together(c, requests, n_diag) * n_diag) : 0;
+    return cts * ct_bytes(c) + std::max(series, cg_workspace_bytes(c->ctx, (uint32_t)together));
 }
 
 static int cpvm_requests(cg_req *c, void *stream, const uint64_t *x, const void *diags, const void *adapters, uint32_t n_adapters,
@@ -368,12 +377,16 @@ static int cpvm_requests(cg_req *c, void *stream, const uint64_t *x, const void 
     auto take = [&](size_t cts) { char *p = at; at += cts * ct; return p; };
     uint64_t *copies = reinterpret_cast<uint64_t *>(take((size_t)requests * (n_diag - 1)));
     double *f = reinterpret_cast<double *>(take((size_t)requests * n_diag));
-    uint64_t *xa = reinterpret_cast<uint64_t *>(take(batch)), *xb = reinterpret_cast<uint64_t *>(take(batch));
+    uint64_t *xa = reinterpret_cast<uint64_t *>(take(batch)), *xb = reinterpret_cast<uint64_t *>(take(std::min(batch, most_together(c))));
     void *rest = at;
+    const size_t words = ct / 8;
     if (n_diag > 1) {
         uint32_t gs[64], e = 1;
         for (uint32_t i = 1; i < n_diag; i++) gs[i - 1] = e = e * 3 % (2u * (uint32_t)c->N);
-        CG_TRY(cg_rotate_hoisted(c->ctx, stream, x, n_diag - 1, gs, gk_copies, copies, requests, rest));
+        for (uint32_t r = 0, n; r < requests; r += n) {
+            n = series_together(c, requests - r, n_diag);
+            CG_TRY(cg_rotate_hoisted(c->ctx, stream, x + r * words, n_diag - 1, gs, gk_copies, copies + (size_t)r * (n_diag - 1) * words, n, rest));
+        }
     }
     CG_TRY(CG_ROWS(c, (size_t)requests * n_diag * 2 * c->k, stream, (x, copies, f, (int)n_diag, c->T), copies_kernel));
     const uint32_t blocks = (uint32_t)(c->N / (2 * PRODUCT_THREADS)) * c->k * requests;
@@ -390,10 +403,9 @@ static int cpvm_requests(cg_req *c, void *stream, const uint64_t *x, const void 
     default: CG_TRY(launch(products_kernel<8, false>, dim3(grid), PRODUCT_THREADS, 0, stream, A, c->T));
     }
     CG_TRY(CG_ROWS(c, (size_t)batch * 2 * c->k, stream, (reinterpret_cast<double *>(xa), c->T), sums_kernel));
-    const size_t words = ct / 8;
     for (uint32_t at_unit = 0, n; at_unit < batch; at_unit += n) {
-        n = round_bits ? fold_together(c, batch - at_unit) : batch;
-        uint64_t *cur = xa + at_unit * words, *next = xb + at_unit * words;
+        n = round_bits ? fold_together(c, batch - at_unit) : std::min(batch - at_unit, most_together(c));
+        uint64_t *cur = xa + at_unit * words, *next = xb;
         for (size_t r = 0, first = 0; r < counts.size(); first += counts[r], r++) {
             uint64_t *to = r + 1 == counts.size() ? out + at_unit * words : next;
             if (round_bits) CG_TRY(cg_rotate_sum_hoisted(c->ctx, stream, cur, counts[r], elts.data() + first, gk_block + first, to, n, rest));
@@ -415,7 +427,10 @@ CG_API int cg_cpvm_requests(cg_req *c, void *stream, const uint64_t *x, const vo
     CG_REQUIRE(round_bits <= 7 && gk_block && (n_diag == 1 || gk_copies) && here(c));
     for (uint32_t i = 0; i + 1 < n_diag; i++) CG_REQUIRE(aligned(gk_copies[i]));
     const size_t n_ws = cg_cpvm_requests_workspace_bytes(c, requests, units, n_diag), n_out = ct_bytes(c) * requests * units;
+    const size_t n_diags = row_bytes(c) * c->k * units * n_diag;
     CG_REQUIRE(!overlap(x, ct_bytes(c) * requests, out, n_out) && !overlap(ws, n_ws, out, n_out) && !overlap(ws, n_ws, x, ct_bytes(c) * requests));
+    CG_REQUIRE(!overlap(diags, n_diags, out, n_out) && !overlap(diags, n_diags, ws, n_ws));
+    CG_REQUIRE(!n_adapters || (!overlap(adapters, n_diags * n_adapters, out, n_out) && !overlap(adapters, n_diags * n_adapters, ws, n_ws)));
     try {
         return cpvm_requests(c, stream, x, diags, adapters, n_adapters, pick, requests, units, n_diag, d2, round_bits, gk_copies, gk_block,
                              out, ws);

@@ -217,7 +217,8 @@ def test_projections_without_adapters_are_those_of_one_request():
 
 
 @pytest.mark.parametrize("name,requests,units,d1,bits", [("C2", 9, 8, 64, 3), ("C2", 12, 12, 64, 3), ("C2", 8, 36, 64, 4), ("C2", 1, 576, 64, 3),
-                                                        ("C1", 13, 41, 64, 3), ("C5", 9, 4, 64, 3), ("C2", 17, 1, 768, 0)])
+                                                        ("C1", 13, 41, 64, 3), ("C5", 9, 4, 64, 3), ("C2", 17, 1, 768, 0),
+                                                        ("C1", 61, 36, 64, 3), ("C1", 140, 1, 768, 3)])
 def test_large_calls_are_the_small_ones(name, requests, units, d1, bits):
     """Calls whose rounds are cut into whole rounds of the compute units and the rest, with adapters: each request against the call
     for one request with its adapter's diagonals added to the base's."""

@@ -102,6 +102,9 @@ def _child(lib):
     assert f.cg_cpvm_requests_workspace_bytes(h, u32(0), u32(1), u32(1)) == f.cg_cpvm_requests_workspace_bytes(h, u32(1), u32(1), u32(0)) == 0
     assert f.cg_cpvm_prepare_workspace_bytes(h, u32(2), u32(100), u32(64), u32(0)) == 0
     assert f.cg_cpvm_prepare_workspace_bytes(h, u32(2), u32(100), u32(64), u32(1)) >= 4 * 2 * 100 * 64
+    # scratch of large calls: the units' own ciphertexts, and a bounded part for those that go together
+    ws = lambda r, u: f.cg_cpvm_requests_workspace_bytes(h, u32(r), u32(u), u32(1))
+    got["ciphertexts a unit beyond"] = (ws(1, 60000) - ws(1, 50000)) / 10000 / (2 * 2 * 4096 * 8)
     assert f.cg_req_destroy(h) == 0 and f.cg_req_destroy(None) == 0
     # creation
     ctx = lib.create(prm)
@@ -153,6 +156,10 @@ def test_what_is_refused_launches_nothing(child):
 def test_diagonals_of_a_matrix(child):
     # N = 4096: tiles of 128 (at least N / d2 = 64 and d1), 1024, 2048; none beyond a slot row, or beyond 64 diagonals
     assert child["n_diag"] == [1, 16, 32, 0, 64, 0, 0]
+
+
+def test_scratch_of_large_calls_is_bounded(child):
+    assert child["ciphertexts a unit beyond"] == 1
 
 
 def test_handles_need_the_contexts_parameters_and_a_modulus_with_slots(child):
