@@ -349,6 +349,20 @@ CG_API size_t cg_cpvm_requests_workspace_bytes(const cg_req *c, uint32_t request
     return cts * ct_bytes(c) + std::max(series, cg_workspace_bytes(c->ctx, (uint32_t)together));
 }
 
+// A quarter as many rows as compute units, and each is taken in four parts (us a projection of one request, whole rows / parts: N = 8192, 48 rows, 3 matrices
+// 114.3 / 113.3, 12 151.4 / 150.2; N = 16384, 48 rows, 3 matrices 250.5 / 245.1; halves, and parts of the sums' rows, are within 0.5 % either way, as is all at N = 4096).
+template <int LOGN> static int copies_in_parts(const cg_req *c, void *s, const LdCopies &ld, double *f, size_t rows)
+{
+    return launch(ntt_fwd_part_kernel<LOGN, 2, LdCopies, StF64Red>, dim3((unsigned)rows * 4), 1u << (LOGN - 5), 0, s, ld, StF64Red{f, LOGN}, c->T.tw, c->T.C,
+                  (int)rows);
+}
+static int transform_copies(const cg_req *c, void *s, const LdCopies &ld, double *f, size_t rows)
+{
+    if (c->logn == 13 && 4 * rows <= (size_t)c->n_cu) return copies_in_parts<13>(c, s, ld, f, rows);
+    if (c->logn == 14 && 4 * rows <= (size_t)c->n_cu) return copies_in_parts<14>(c, s, ld, f, rows);
+    return CG_ROWS(c, rows, s, (ld, f, c->T), copies_kernel);
+}
+
 static int cpvm_requests(cg_req *c, void *stream, const uint64_t *x, const void *diags, const void *adapters, uint32_t n_adapters,
                          const int32_t *pick, uint32_t requests, uint32_t units, uint32_t n_diag, uint32_t d2,
                          uint32_t round_bits, const void *const *gk_copies, const void *const *gk_block, uint64_t *out, void *ws)
@@ -388,7 +402,7 @@ static int cpvm_requests(cg_req *c, void *stream, const uint64_t *x, const void 
             CG_TRY(cg_rotate_hoisted(c->ctx, stream, x + r * words, n_diag - 1, gs, gk_copies, copies + (size_t)r * (n_diag - 1) * words, n, rest));
         }
     }
-    CG_TRY(CG_ROWS(c, (size_t)requests * n_diag * 2 * c->k, stream, (x, copies, f, (int)n_diag, c->T), copies_kernel));
+    CG_TRY(transform_copies(c, stream, LdCopies{x, copies, (int)n_diag, c->k, c->logn}, f, (size_t)requests * n_diag * 2 * c->k));
     const uint32_t blocks = (uint32_t)(c->N / (2 * PRODUCT_THREADS)) * c->k * requests;
     // three workgroups to a compute unit are resident (one to twelve are within 1 %)
     const uint32_t parts0 = std::min(units, std::max(1u, 3 * (uint32_t)c->n_cu / blocks)), per = (units + parts0 - 1) / parts0;

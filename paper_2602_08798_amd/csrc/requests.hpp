@@ -266,16 +266,29 @@ low_rank_kernel(const int64_t *__restrict__ w, const int64_t *__restrict__ a, co
 // ---------------------------------------------------------------------------
 // The copies of all tokens, transformed: row (r, c, component, prime), copy 0 being the token itself.  768 rows of 8192 (16 requests) 24 us.
 // ---------------------------------------------------------------------------
+struct LdCopies {
+    static constexpr int kRaw = 1;
+    static constexpr bool kScatter = false;
+    const uint64_t *x, *copies;
+    int n_diag, k, logn;
+    __device__ __forceinline__ int prime(int row, const DevConst *) const { return row % k; }
+    __device__ __forceinline__ int dst_limb(int row, const DevConst *) const { return row; }
+    __device__ __forceinline__ const uint64_t *row(int row) const
+    {
+        const int cp = row / (2 * k), r = cp / n_diag, c = cp % n_diag, in_ct = row % (2 * k);
+        return c ? copies + ((size_t)((r * (n_diag - 1) + c - 1) * 2 * k + in_ct) << logn) : x + ((size_t)(r * 2 * k + in_ct) << logn);
+    }
+    __device__ __forceinline__ void fetch(int at, int idx, const DevConst *, uint64_t *raw) const { raw[0] = at32(row(at), idx); }
+    __device__ __forceinline__ double finish(const uint64_t *raw, int, int, const ModD, const DevConst *) const { return u64_to_f64(raw[0]); }
+};
 template <int LOGN, int E>
 __global__ void __launch_bounds__((1 << LOGN) / E, (min_waves<LOGN, E>()))
-copies_kernel(const uint64_t *__restrict__ x, const uint64_t *__restrict__ copies, double *__restrict__ out, int n_diag, Tables T)
+copies_kernel(LdCopies ld, double *__restrict__ out, Tables T)
 {
     __shared__ __align__(16) double lds[lds_doubles<LOGN>()];
     constexpr int TH = (1 << LOGN) / E;
-    const int tid = threadIdx.x, k = T.k;
-    const int row = (int)blockIdx.x, i = row % k, cp = row / (2 * k), r = cp / n_diag, c = cp % n_diag;
-    const int in_ct = row % (2 * k);
-    const uint64_t *src = c ? copies + ((size_t)((r * (n_diag - 1) + c - 1) * 2 * k + in_ct) << LOGN) : x + ((size_t)(r * 2 * k + in_ct) << LOGN);
+    const int tid = threadIdx.x, row = (int)blockIdx.x, i = row % T.k;
+    const uint64_t *src = ld.row(row);
     const ModD m = T.C->mod[i];
     double v[E], w[E];
 #pragma unroll
