@@ -108,7 +108,7 @@ __device__ __forceinline__ void small_inv_row(double *lds, double *out, int tid,
 // values in the order of the transform's outputs; its results are centred in registers and go through one forward
 // transform per ciphertext prime without leaving the workgroup.  Values are read in the order of the slots, which their
 // sources hold side by side, and put in their places in LDS (read in the order of the places 300 plaintexts took 52.4 us, now 47.9).
-// Bound by vector issue: 1000 plaintexts of N = 8192 and three primes take 91 us, 22.8 ns a row transform, their 262 MB at the rate of a
+// Bound by vector issue: 1000 plaintexts of N = 8192 and three primes take 88 us, 22.1 ns a row transform, their 262 MB at the rate of a
 // copy would take 49; in 75 registers with one workgroup to a unit 102, with the interpolation by the passes for 50-bit primes 93.6.  One plaintext
 // takes 12.0 us with its primes on workgroups of their own, one after the other 22.5.
 // ---------------------------------------------------------------------------
@@ -180,7 +180,10 @@ encode_kernel(LD ld, void *__restrict__ out, Tables T, int whole, int split)
                 w[it] = (double)lift[it];
             }
             double *row = static_cast<double *>(out) + ((size_t)(b * k + i) << LOGN);
-            fwd_row<LOGN, E, false, false, 1, 1>(lds, w, v, tid, T.tw + ((size_t)i << LOGN), m);
+            // Two workgroups to a unit fall out of step with priorities in the passes, one's exchanges under the other's butterflies: one row 12.1 ->
+            // 11.7, 256 rows 27.4 -> 27.0, 1000 rows 90.0 -> 88.4 (N = 8192), 31.7 -> 31.3 (1000, N = 4096). At N = 16384 a workgroup has its unit for
+            // itself, and 128 rows take 51.6 with them, 49.4 without.
+            fwd_row<LOGN, E, false, (LOGN < 14), 1, 1>(lds, w, v, tid, T.tw + ((size_t)i << LOGN), m);
 #pragma unroll
             for (int it = 0; it < E; it += 2)
                 put_lane(reinterpret_cast<cg_double2v *>(row) + 32 * it, chunk_elem<E>(tid, 0) / 2,
