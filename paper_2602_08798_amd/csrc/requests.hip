@@ -444,7 +444,8 @@ CG_API int cg_cpvm_requests(cg_req *c, void *stream, const uint64_t *x, const vo
     const size_t n_diags = row_bytes(c) * c->k * units * n_diag;
     CG_REQUIRE(!overlap(x, ct_bytes(c) * requests, out, n_out) && !overlap(ws, n_ws, out, n_out) && !overlap(ws, n_ws, x, ct_bytes(c) * requests));
     CG_REQUIRE(!overlap(diags, n_diags, out, n_out) && !overlap(diags, n_diags, ws, n_ws));
-    CG_REQUIRE(!n_adapters || (!overlap(adapters, n_diags * n_adapters, out, n_out) && !overlap(adapters, n_diags * n_adapters, ws, n_ws)));
+    CG_REQUIRE(!n_adapters || (!overlap(adapters, n_diags * n_adapters, out, n_out) && !overlap(adapters, n_diags * n_adapters, ws, n_ws) &&
+                               !overlap(pick, 4 * (size_t)requests, out, n_out) && !overlap(pick, 4 * (size_t)requests, ws, n_ws)));
     try {
         return cpvm_requests(c, stream, x, diags, adapters, n_adapters, pick, requests, units, n_diag, d2, round_bits, gk_copies, gk_block,
                              out, ws);
@@ -463,7 +464,10 @@ static int add_bias(cg_req *c, void *stream, const uint64_t *in, uint32_t groups
     CG_REQUIRE(groups >= 1 && heads >= 1 && n_cts >= 1 && n_buckets >= 1 && n_buckets <= 4096);
     CG_REQUIRE(in_one_call((uint64_t)groups * heads) && in_one_call((uint64_t)groups * heads * n_cts));
     const uint32_t units = groups * heads * n_cts;
-    CG_REQUIRE(in == out || !overlap(in, ct_bytes(c) * units, out, ct_bytes(c) * units));
+    const size_t n_out = ct_bytes(c) * units;
+    CG_REQUIRE(in == out || !overlap(in, n_out, out, n_out));
+    CG_REQUIRE((!pos || !overlap(pos, 4 * (size_t)groups, out, n_out)) && !overlap(table, 8 * (size_t)n_buckets * heads, out, n_out) &&
+               !overlap(edges, 4 * (size_t)n_buckets, out, n_out));
     const BiasArgs A{in, out, pos, table, edges, (int)n_buckets, (int)heads, (int)n_cts, log2_of(d2)};
     const size_t lds = (size_t)c->N / d2 * sizeof(float);
 #define CG_BIAS(K) launch(bias_kernel<K, 2>, dim3(units * (unsigned)(c->N / (4 * BIAS_THREADS))), BIAS_THREADS, lds, stream, A, c->T)
@@ -502,7 +506,9 @@ CG_API int cg_kv_append_requests(cg_req *c, void *stream, uint64_t *cache, uint3
     CG_REQUIRE(requests >= 1 && per >= 1 && in_one_call((uint64_t)requests * per) && cache_stride_cts >= 1 && row_stride_cts >= per);
     CG_REQUIRE(power_of_two(d2) && d2 <= (uint32_t)c->N / 2);
     const size_t caches = (size_t)requests * per, n_rows = ((size_t)(requests - 1) * row_stride_cts + per) * ct_bytes(c);
-    CG_REQUIRE(!overlap(cache, caches * cache_stride_cts * ct_bytes(c), rows, n_rows));
+    const size_t n_cache = caches * cache_stride_cts * ct_bytes(c);
+    CG_REQUIRE(!overlap(cache, n_cache, rows, n_rows) && !overlap(cache, n_cache, masks, row_bytes(c) * c->k * (c->N / d2)) &&
+               !overlap(cache, n_cache, lens, 4 * (size_t)requests));
     const AppendArgs A{cache, rows, static_cast<const double *>(masks), lens, (int)per, log2_of((uint32_t)c->N / d2), cache_stride_cts,
                        row_stride_cts};
     return CG_ROWS(c, caches * 2 * c->k, stream, (A, c->T), append_kernel);

@@ -96,7 +96,18 @@ def _child(lib):
     got["missing block key"] = f.cg_cpvm_requests(h, *few)
     assert f.cg_cpvm_requests(h, None, d, d, None, u32(0), None, u32(1), u32(1), u32(1), u32(64), u32(0), None, KEYS, far, farther) == 0
     assert f.cg_cpvm_prepare(h, None, d, None, None, u32(1), u32(1), u32(100), u32(64), u32(0), far, None) == 0
-    assert f.cg_score_bias(h, None, d, u32(1), u32(1), u32(1), u32(64), at4, d, at4, u32(1), d) == 0
+    assert f.cg_score_bias(h, None, far, u32(1), u32(1), u32(1), u32(64), at4, d, at4, u32(1), far) == 0
+    # small arrays that the call would write over while it reads them: within the output or the workspace, to their last entry
+    within, last4 = vp(far.value + 64), vp(far.value - 4)
+    for name, at, values in (("cg_cpvm_requests", 5, [within, vp(far.value - 8), vp(farther.value + 64)]), ("cg_score_bias", 6, [within, last4]),
+                             ("cg_score_bias", 7, [within, vp(far.value - 32)]), ("cg_score_bias", 8, [within, vp(far.value - 8)]),
+                             ("cg_prompt_bias", 5, [within]), ("cg_prompt_bias", 6, [within]),
+                             ("cg_kv_append_requests", 5, [within, last4]), ("cg_kv_append_requests", 8, [within, vp(far.value - 16)])):
+        for v in values:
+            bad = base[name][:at] + [v] + base[name][at + 1:]
+            lib.stub.stub_log_clear()
+            if getattr(f, name)(h, *bad) != -1 or lib.stub.stub_log_size():
+                got["accepted"].append([name, at, "overlaps", str(v)])
     # sizes
     got["n_diag"] = [f.cg_cpvm_diagonals(h, u32(a), u32(b)) for a, b in ((1, 64), (768, 64), (2048, 64), (2049, 64), (2048, 128), (2048, 256), (100, 48))]
     assert f.cg_cpvm_requests_workspace_bytes(h, u32(0), u32(1), u32(1)) == f.cg_cpvm_requests_workspace_bytes(h, u32(1), u32(1), u32(0)) == 0
@@ -137,7 +148,7 @@ def _unreached(lib):
                     go("cg_cpvm_requests", d, d, None, u32(0), None, u32(2), b, u32(n_diag), u32(64), u32(3), KEYS, KEYS, far, farther)
                 for d2 in (2, 64, 1024):
                     go("cg_score_bias", d, b, u32(1), u32(1), u32(d2), at4, d, at4, u32(3), far)
-                    go("cg_score_bias", d, b, u32(1), u32(1), u32(d2), at4, d, at4, u32(3), d)
+                    go("cg_score_bias", far, b, u32(1), u32(1), u32(d2), at4, d, at4, u32(3), far)
                 go("cg_kv_append_requests", far, u32(2), b, u32(2), at4, d, u32(2), d, u32(64))
             assert f.cg_req_destroy(h) == 0
     return sorted(set(lib.own) - seen)
