@@ -15,7 +15,8 @@
  *               plaintext is its value at zeta^e, e = 3^i for s = i < N/2 and -3^i for s = N/2 + i (mod 2N),
  *               zeta the smallest primitive 2N-th root of unity modulo t.
  *   int32       arrays of one entry per request or bucket need only 4-byte alignment.
- *   device      every call needs the handle's device to be the current one (CG_EINVAL otherwise).
+ *   device      every call needs the handle's device to be the current one (CG_EINVAL otherwise; for create it
+ *               is the context's, and destroy waits for the current one).
  *   threads     a handle holds constant tables only: calls may run at once, with workspaces of their own.
  *   capture     every call but create and destroy can be captured.
  */
@@ -65,7 +66,7 @@ int cg_cpvm_prepare(cg_req *req, void *stream, const int64_t *w_dev, const int64
  * [n_adapters][units][n_diag] (of A B alone, from cg_cpvm_prepare without W) or NULL with n_adapters = 0;
  * pick_dev: int32[requests], read when the call runs: any value outside [0, n_adapters) means no adapter
  * (may be NULL when n_adapters is 0).  out_dev: [requests][units] ciphertexts.  Without an adapter the
- * results are those of cg_cpvm_hoisted for each request.  requests units <= 65536, requests (n_diag - 1)
+ * results are those of cg_cpvm_hoisted for each request.  requests units <= 65536, requests n_diag
  * <= 65536.  ws_dev: cg_cpvm_requests_workspace_bytes(...) bytes. */
 size_t cg_cpvm_requests_workspace_bytes(const cg_req *req, uint32_t requests, uint32_t units, uint32_t n_diag);
 int cg_cpvm_requests(cg_req *req, void *stream, const uint64_t *x_dev, const void *diags_dev,

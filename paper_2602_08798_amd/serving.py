@@ -15,8 +15,9 @@ _I64, _F64, _I32 = torch.int64, torch.float64, torch.int32
 
 
 def _count(x) -> int:
+    """A size as the entry points take it, in 32 bits; anything else is 0, which none of them accepts."""
     x = int(x)
-    return x if x > 0 else 0
+    return x if 0 < x < 1 << 32 else 0
 
 
 class Requests:
@@ -40,7 +41,8 @@ class Requests:
 
     def close(self):
         if getattr(self, "h", None):
-            self.lib.dll.cg_req_destroy(self.h)
+            with torch.cuda.device(self.device):
+                self.lib.dll.cg_req_destroy(self.h)
             self.h = None
 
     def __del__(self):
@@ -143,7 +145,7 @@ class Requests:
         """y[r][u] = x_r (W_u + the adapter pick[r] asks for), as Context.cpvm_hoisted computes it for one request: adapters
         prepared [n_adapters][units][n_diag] without W, pick int32 [requests] on the GPU (anything else than 0 .. n_adapters - 1:
         none)."""
-        ctx, R, U, D = self.ctx, _count(requests), _count(units), _count(n_diag)
+        ctx, R, U, D, d2 = self.ctx, _count(requests), _count(units), _count(n_diag), _count(d2)
         out = ctx.empty_ct(R, U) if out is None else out
         ctx._need_keys(list(gk_copies) + list(gk_block))
         if len(gk_copies) != max(0, D - 1):
@@ -166,20 +168,22 @@ class Requests:
     # ---- position biases ----
     def _tables(self, table, edges, heads):
         n = edges.numel()
-        return self._at(table, _I64, n * _count(heads), "table"), self._at(edges, _I32, 1, "edges"), n
+        return self._at(table, _I64, n * heads, "table"), self._at(edges, _I32, 1, "edges"), n
 
     def score_bias(self, scores, requests, heads, n_cts, d2, pos, table, edges, out=None):
         """scores [requests][heads][n_cts] + the bias of every token's distance to pos[request]; table int64 [buckets][heads], edges int32
         [buckets] ascending.  out=scores works in place."""
-        units = _count(requests) * _count(heads) * _count(n_cts)
+        requests, heads, n_cts = _count(requests), _count(heads), _count(n_cts)
+        units = requests * heads * n_cts
         out = torch.empty_like(scores) if out is None else out
-        self._call("cg_score_bias", self._cts(scores, units, "scores"), requests, heads, n_cts, d2,
-                   self._at(pos, _I32, _count(requests), "pos"), *self._tables(table, edges, heads), self._cts(out, units, "out"))
+        self._call("cg_score_bias", self._cts(scores, units, "scores"), requests, heads, n_cts, _count(d2),
+                   self._at(pos, _I32, requests, "pos"), *self._tables(table, edges, heads), self._cts(out, units, "out"))
         return out
 
     def prompt_bias(self, diagonals, prompts, heads, d2, table, edges, out=None):
         """The same for the diagonals of prefill_qk, [prompts][heads][N / d2]."""
-        units = _count(prompts) * _count(heads) * (self.n // max(1, _count(d2)))
+        prompts, heads, d2 = _count(prompts), _count(heads), _count(d2)
+        units = prompts * heads * (self.n // max(1, d2))
         out = torch.empty_like(diagonals) if out is None else out
         self._call("cg_prompt_bias", self._cts(diagonals, units, "diagonals"), prompts, heads, d2, *self._tables(table, edges, heads),
                    self._cts(out, units, "out"))
@@ -189,8 +193,8 @@ class Requests:
     def kv_append_requests(self, cache, cache_stride_cts, requests, per, lens, rows, masks, d2, row_stride_cts=None):
         """Every request's `per` new rows into its caches at its own length: cache [requests][per][cache_stride_cts], lens int32
         [requests] on the GPU (below 0, or a full cache: left as it is), rows [requests][row_stride_cts or per]."""
-        R, P = _count(requests), _count(per)
+        R, P, stride, d2 = _count(requests), _count(per), _count(cache_stride_cts), _count(d2)
         gap = P if row_stride_cts is None else _count(row_stride_cts)
-        self._call("cg_kv_append_requests", self._cts(cache, R * P * _count(cache_stride_cts), "cache"), cache_stride_cts, R, P,
+        self._call("cg_kv_append_requests", self._cts(cache, R * P * stride, "cache"), stride, R, P,
                    self._at(lens, _I32, R, "lens"), self._cts(rows, max(0, R - 1) * gap + P, "rows"), gap,
-                   self._plains(masks, self.n // max(1, _count(d2)), "masks"), d2)
+                   self._plains(masks, self.n // max(1, d2), "masks"), d2)

@@ -499,3 +499,32 @@ def test_refusals():
             rq.kv_append_requests(cache, *bad)
     with pytest.raises(CgError):
         rq.kv_append_requests(cache, 2, 2, 1, lens, x, masks, 64, row_stride_cts=0)
+
+
+@pytest.mark.parametrize("wrap", [1 << 32, -(1 << 32)])
+def test_sizes_that_would_pass_in_their_low_32_bits_are_refused(wrap):
+    import torch
+    from paper_2602_08798_amd.binding import CgError
+    env = _env("C1")
+    rq, n = env.rq, env.n
+    a, b = _ints(np.zeros((1, 100, 4))), _ints(np.zeros((2, 4, 64)))
+    x, plain, many = env.dev(env.cts(1, 2)), rq.slots_prepare(_ints(np.zeros((n // 64, n)))), env.dev(env.cts(2, n // 64))
+    copies, block, _ = _projection(env, 100, 64, 3, 500)
+    C = attention.cpvm_shape(n, 100, 64)[2]
+    table, edges, pos, lens = _ints([[1], [2]]), _lens([0, 3]), _lens([1, 1]), _lens([0, 0])
+    cache = env.dev(env.cts(3, 4))
+    out = torch.empty(4 * rq.k * n, dtype=torch.float64, device="cuda")
+    calls = [lambda *s: rq.cpvm_prepare(s[0], s[1], s[2], a=a, b=b, a_group=s[3], out=out),
+             lambda *s: rq.cpvm_requests(x, plain, s[0], s[1], s[2], s[3], copies, block, block_round_bits=3, out=cache),
+             lambda *s: rq.score_bias(x, s[0], s[1], s[2], s[3], pos, table, edges),
+             lambda *s: rq.prompt_bias(many, s[0], s[1], s[2], table, edges),
+             lambda *s: rq.kv_append_requests(cache, s[0], s[1], s[2], lens, x, plain, s[3], row_stride_cts=s[4])]
+    sizes = [(2, 100, 64, 2), (1, 1, C, 64), (2, 1, 1, 64), (1, 1, 64), (2, 2, 1, 64, 1)]
+    for call, good in zip(calls, sizes):
+        call(*good)
+        for at in range(len(good)):
+            bad = list(good)
+            bad[at] += wrap
+            with pytest.raises(CgError):
+                call(*bad)
+    assert rq.cpvm_diagonals(100 + wrap, 64) == rq.cpvm_diagonals(100, 64 + wrap) == 0
