@@ -528,3 +528,41 @@ def test_sizes_that_would_pass_in_their_low_32_bits_are_refused(wrap):
             with pytest.raises(CgError):
                 call(*bad)
     assert rq.cpvm_diagonals(100 + wrap, 64) == rq.cpvm_diagonals(100, 64 + wrap) == 0
+
+
+def test_offsets_beyond_32_bits():
+    """Caches, scores, plaintexts and units of more than 2^32 bytes: what lies behind, against the small calls."""
+    import torch
+    env = _env("C1")
+    rq, n, k, d2 = env.rq, env.n, env.k, 64
+    B, ct = n // d2, 2 * k * n
+    far = (5 << 30) // (8 * ct)                       # ciphertexts in 5 GiB
+    rows = env.dev(env.cts(60, 2))
+    masks = env.ctx.plain_prepare(env.dev(np.random.default_rng(1).integers(0, env.prm.t, (B, n)).astype(np.uint64)))
+    say(f"append: stride {far}")
+    old = env.dev(env.cts(61, 2)).view(2, 1, ct)
+    cache = torch.zeros((2, far, ct), dtype=torch.int64, device="cuda")
+    cache[:, far - 1] = old[:, 0]
+    rq.kv_append_requests(cache, far, 2, 1, _lens([B * far - 1, B * (far - 1)]), rows, masks, d2)
+    rq.kv_append_requests(old, 1, 2, 1, _lens([B - 1, 0]), rows, masks, d2)
+    assert torch.equal(cache[:, far - 1:], old) and not cache[:, :far - 1].any()
+    say(f"score_bias: {far} ciphertexts, in place")
+    scores, few = cache[0], env.dev(env.cts(62, 3)).view(3, ct)
+    table, edges = _bias_case(env, 1, 9, 3)
+    scores[far - 3:] = few
+    rq.score_bias(scores, 1, 1, far, d2, _lens([B * (far - 2) + 5]), _ints(table), _lens(edges), out=scores)
+    assert torch.equal(scores[far - 3:], rq.score_bias(few, 1, 1, 3, d2, _lens([B + 5]), _ints(table), _lens(edges)))
+    del cache, scores
+    torch.cuda.empty_cache()
+    say("slots_prepare: 65536 plaintexts")
+    v = torch.zeros((65536, n), dtype=torch.int64, device="cuda")
+    last = _ints(_slots(n, 9, env.prm.t, 5))
+    v[-9:] = last
+    plain = rq.slots_prepare(v).view(65536, -1)
+    assert torch.equal(plain[-9:], rq.slots_prepare(last).view(9, -1)) and not plain[:-9].any()
+    del v
+    say("cpvm_requests: 65536 units")
+    copies, block, _ = _projection(env, 64, d2, 3, 500)
+    got = rq.cpvm_requests(rows[:1], plain, 1, 65536, 1, d2, copies, block, block_round_bits=3).view(65536, ct)
+    few = rq.cpvm_requests(rows[:1], plain[-9:].contiguous(), 1, 9, 1, d2, copies, block, block_round_bits=3).view(9, ct)
+    assert torch.equal(got[-9:], few) and not got[:-9].any()
