@@ -330,6 +330,7 @@ CG_API int cg_cpvm_prepare(cg_req *c, void *stream, const int64_t *w, const int6
     } else {
         a_group = 1;
     }
+    a_group = std::min(a_group, units);      // (the kernel divides int32, which any larger number need not be)
     const uint32_t row_blocks = (d1 + 63) / 64;
     float *m = static_cast<float *>(ws);
     CG_TRY(launch(low_rank_kernel, dim3(units * row_blocks, (d2 + 63) / 64), 256, 0, stream, w, a, b, m, (int)a_group, (int)d1, log2_of(d2),
