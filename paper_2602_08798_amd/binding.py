@@ -58,8 +58,51 @@ def _params(params) -> _Params:
     return _Params(params.log2n, params.k, params.nsp, params.alpha, int(params.t), q, p)
 
 
+class _Dll(C.CDLL):
+    """The evaluator.  The entry points of libcryptogen_requests.so stand beside its own from their first use on: a program
+    that makes no use of them needs no such library."""
+
+    def __getattr__(self, name):
+        if name not in _REQUEST_SYMBOLS:
+            return super().__getattr__(name)
+        r = _requests_library(self)
+        for each in _REQUEST_SYMBOLS:
+            setattr(self, each, getattr(r, each))
+        return getattr(self, name)
+
+
+def _requests_library(evaluator) -> C.CDLL:
+    """libcryptogen_requests.so with typed entry points, if it calls this evaluator."""
+    if not os.path.exists(_REQUESTS_PATH):
+        raise RuntimeError(f"{_REQUESTS_PATH} is missing: build it with `python -m paper_2602_08798_amd.build`")
+    r = C.CDLL(_REQUESTS_PATH)
+    # The loader knows the evaluator by its soname.  One that was linked without (or a second one) stays unknown to it, and another
+    # copy comes in, which must not be given this one's contexts.
+    if C.cast(r.cg_create, C.c_void_p).value != C.cast(evaluator.cg_create, C.c_void_p).value:
+        raise RuntimeError(f"{_REQUESTS_PATH} calls another copy of the evaluator than {evaluator._name}: link that one with "
+                           "-Wl,-soname,libcryptogen_hip.so, and load no other before it")
+    vp, u32 = C.c_void_p, C.c_uint32
+    for name in _REQUEST_SYMBOLS:
+        getattr(r, name).restype = C.c_int
+    r.cg_req_create.argtypes = [C.POINTER(vp), vp, C.POINTER(_Params)]
+    r.cg_req_destroy.argtypes = [vp]
+    r.cg_slots_encode.argtypes = r.cg_slots_prepare.argtypes = [vp, vp, vp, vp, u32]
+    r.cg_cpvm_diagonals.argtypes = [vp, u32, u32]
+    r.cg_cpvm_diagonals.restype = u32
+    r.cg_cpvm_prepare_workspace_bytes.argtypes = [vp, u32, u32, u32, u32]
+    r.cg_cpvm_prepare_workspace_bytes.restype = C.c_size_t
+    r.cg_cpvm_prepare.argtypes = [vp, vp, vp, vp, vp, u32, u32, u32, u32, u32, vp, vp]
+    r.cg_cpvm_requests_workspace_bytes.argtypes = [vp, u32, u32, u32]
+    r.cg_cpvm_requests_workspace_bytes.restype = C.c_size_t
+    r.cg_cpvm_requests.argtypes = [vp, vp, vp, vp, vp, u32, vp, u32, u32, u32, u32, u32, C.POINTER(vp), C.POINTER(vp), vp, vp]
+    r.cg_score_bias.argtypes = [vp, vp, vp, u32, u32, u32, u32, vp, vp, vp, u32, vp]
+    r.cg_prompt_bias.argtypes = [vp, vp, vp, u32, u32, u32, vp, vp, u32, vp]
+    r.cg_kv_append_requests.argtypes = [vp, vp, vp, u32, u32, u32, vp, vp, u32, vp, u32]
+    return r
+
+
 class Library:
-    """The loaded shared libraries with typed entry points."""
+    """The loaded shared library with typed entry points (those of libcryptogen_requests.so are loaded when they are used first)."""
 
     def __init__(self, path: str = _LIB_PATH):
         if not os.path.exists(path):
@@ -67,7 +110,7 @@ class Library:
                 f"{path} is missing: build it with `python -m paper_2602_08798_amd.build` "
                 "(there is no CPU fallback)")
         self.path = path
-        self.dll = C.CDLL(path)
+        self.dll = _Dll(path)
         vp, u32, i32 = C.c_void_p, C.c_uint32, C.c_int
         d = self.dll
         d.cg_create.argtypes = [C.POINTER(vp), C.POINTER(_Params)]
@@ -131,27 +174,6 @@ class Library:
             if name not in ("cg_workspace_bytes", "cg_decode_step_workspace_bytes", "cg_strerror", "cg_kernel_name",
                             "cg_static_scratch_bytes"):
                 getattr(d, name).restype = i32
-        if not os.path.exists(_REQUESTS_PATH):
-            raise RuntimeError(f"{_REQUESTS_PATH} is missing: build it with `python -m paper_2602_08798_amd.build`")
-        # its entry points beside the evaluator's
-        r = self.requests_dll = C.CDLL(_REQUESTS_PATH)
-        for name in _REQUEST_SYMBOLS:
-            setattr(d, name, getattr(r, name))
-            getattr(d, name).restype = i32
-        d.cg_req_create.argtypes = [C.POINTER(vp), vp, C.POINTER(_Params)]
-        d.cg_req_destroy.argtypes = [vp]
-        d.cg_slots_encode.argtypes = d.cg_slots_prepare.argtypes = [vp, vp, vp, vp, u32]
-        d.cg_cpvm_diagonals.argtypes = [vp, u32, u32]
-        d.cg_cpvm_diagonals.restype = u32
-        d.cg_cpvm_prepare_workspace_bytes.argtypes = [vp, u32, u32, u32, u32]
-        d.cg_cpvm_prepare_workspace_bytes.restype = C.c_size_t
-        d.cg_cpvm_prepare.argtypes = [vp, vp, vp, vp, vp, u32, u32, u32, u32, u32, vp, vp]
-        d.cg_cpvm_requests_workspace_bytes.argtypes = [vp, u32, u32, u32]
-        d.cg_cpvm_requests_workspace_bytes.restype = C.c_size_t
-        d.cg_cpvm_requests.argtypes = [vp, vp, vp, vp, vp, u32, vp, u32, u32, u32, u32, u32, C.POINTER(vp), C.POINTER(vp), vp, vp]
-        d.cg_score_bias.argtypes = [vp, vp, vp, u32, u32, u32, u32, vp, vp, vp, u32, vp]
-        d.cg_prompt_bias.argtypes = [vp, vp, vp, u32, u32, u32, vp, vp, u32, vp]
-        d.cg_kv_append_requests.argtypes = [vp, vp, vp, u32, u32, u32, vp, vp, u32, vp, u32]
 
     def strerror(self, status: int) -> str:
         return self.dll.cg_strerror(status).decode()
