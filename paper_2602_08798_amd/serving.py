@@ -23,7 +23,8 @@ def _count(x) -> int:
 class Requests:
     """The plaintext side of a server: a handle of constant tables beside a Context (whose t must have slots: a prime, 1 mod 2N).
 
-    Its creation synchronises; every other method only enqueues, and can be captured.  Close it before its context."""
+    Its creation synchronises; every other method only enqueues, and can be captured.  Threads may call one handle at once, on
+    any streams: every call takes scratch of its own.  Close it before its context."""
 
     def __init__(self, ctx: Context):
         self.ctx, self.lib = ctx, ctx.lib
@@ -32,7 +33,6 @@ class Requests:
         self.n, self.k = ctx.n, ctx.k
         self._ct = 2 * self.k * self.n
         self._calls = {name: getattr(self.lib.dll, name) for name in _REQUEST_SYMBOLS}
-        self._ws = {}
         self.h = None
         h, prm = C.c_void_p(), _params(ctx.params)
         with torch.cuda.device(self.device):
@@ -83,17 +83,9 @@ class Requests:
         return torch.empty(shape, dtype=dtype, device=self.device)
 
     def _workspace(self, need: int) -> torch.Tensor:
-        """Scratch that is the current stream's alone.  A captured call has its own, from the graph's pool: what an eager call keeps
-        may be replaced by a larger one while the graph lives."""
-        with torch.cuda.device(self.device):
-            if torch.cuda.is_current_stream_capturing():
-                return self._empty(need, torch.uint8)
-        key = self.ctx.stream
-        ws = self._ws.get(key)
-        if ws is None or ws.numel() < need:
-            self._ws.pop(key, None)
-            ws = self._ws[key] = self._empty(need, torch.uint8)
-        return ws
+        """Scratch of one call, which keeps it until everything is enqueued: the allocator gives the memory to what is enqueued behind, and never
+        to a call that another thread makes at the same time on the same stream."""
+        return self._empty(need, torch.uint8)
 
     # ---- slots ----
     def _batch(self, slots):
