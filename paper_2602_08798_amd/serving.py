@@ -51,9 +51,17 @@ class Requests:
         except Exception:
             pass
 
-    def _call(self, name, *args):
+    def _open(self, name):
         if not self.h or not self.ctx.h:
             raise CgError(f"{name}: the handle or its context is closed")
+        return self.h
+
+    def _ask(self, name, *args) -> int:
+        """The bytes of scratch that a call needs, which the handle asks its context for."""
+        return int(self._calls[name](self._open(name), *args))
+
+    def _call(self, name, *args):
+        self._open(name)
         if _current_device() == self._index:
             status = self._calls[name](self.h, _raw_stream(self._index), *args)
         else:
@@ -126,7 +134,7 @@ class Requests:
                 raise CgSizeError(f"a {tuple(a.shape)} and b {tuple(b.shape)} do not make {units} matrices of {d1} x {d2}")
         plains = units * self.cpvm_diagonals(d1, d2)
         out = self._empty(plains * self.k * self.n, _F64) if out is None else out
-        need = int(self.lib.dll.cg_cpvm_prepare_workspace_bytes(self.h, units, d1, d2, rank))
+        need = self._ask("cg_cpvm_prepare_workspace_bytes", units, d1, d2, rank)
         ws = self._workspace(need) if need else None
         self._call("cg_cpvm_prepare", self._at(w, _I64, units * d1 * d2, "w"), self._at(a, _I64, 0, "a"), self._at(b, _I64, 0, "b"), units, a_group,
                    d1, d2, rank, self._plains(out, plains, "out"), 0 if ws is None else ws.data_ptr())
@@ -153,7 +161,7 @@ class Requests:
         args = (self._cts(x, R, "x"), self._plains(diags, U * D, "diags"), self._plains(adapters, 0, "adapters"), n_adapters,
                 self._at(pick, _I32, R, "pick") if n_adapters else 0, R, U, D, d2, block_round_bits,
                 ctx._keys(gk_copies) if len(gk_copies) else None, ctx._keys(gk_block), self._cts(out, R * U, "out"))
-        ws = self._workspace(int(self.lib.dll.cg_cpvm_requests_workspace_bytes(self.h, R, U, D)))
+        ws = self._workspace(self._ask("cg_cpvm_requests_workspace_bytes", R, U, D))
         self._call("cg_cpvm_requests", *args, ws.data_ptr())
         return out
 

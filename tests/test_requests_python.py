@@ -61,3 +61,13 @@ def test_calls_made_at_once_have_scratch_of_their_own(requests, name, call):
     call(requests)
     ws = [args[-1] for made, args in requests.dll.made if made == name]
     assert len(ws) == 2 and 0 not in ws and ws[0] != ws[1]
+
+
+@pytest.mark.parametrize("closed", ["handle", "context"])
+def test_what_is_closed_is_not_asked_anything(requests, closed):
+    """No entry point sees a handle whose context is gone: the size of the scratch is asked of both."""
+    setattr(requests if closed == "handle" else requests.ctx, "h", None)
+    for call in (prepare, project):
+        with pytest.raises(CgError):
+            call(requests)
+    assert {name for name, _ in requests.dll.made} <= {"cg_cpvm_diagonals"}       # (a matter of the ring alone; 0 without a handle)
