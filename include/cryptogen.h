@@ -94,6 +94,9 @@ typedef struct {
 int cg_create(cg_ctx **out, const cg_params *prm);
 int cg_destroy(cg_ctx *ctx);
 int cg_get_sizes(const cg_ctx *ctx, cg_sizes *out);
+/* CG_OK if the context was created with these parameters (p may be NULL: the special primes are then not
+ * compared) and its tables are on the current device, CG_EINVAL otherwise. */
+int cg_check_params(const cg_ctx *ctx, const cg_params *prm);
 /* Bytes of caller-provided scratch ("ws") that any call below needs for the
  * given batch; contents are undefined between calls. */
 size_t cg_workspace_bytes(const cg_ctx *ctx, uint32_t batch);

@@ -32,8 +32,9 @@ extern "C" {
 typedef struct cg_req cg_req;
 
 /* Tables for a context and the parameters it was created with (both stay the caller's; the context must
- * outlive the handle).  t must be a prime with t = 1 mod 2N: only such a modulus has N slots
- * (CG_EINVAL otherwise).  Synchronises the device, as does cg_req_destroy. */
+ * outlive the handle; others than the context's, or another current device than its own, are CG_EINVAL).  t must
+ * be a prime with t = 1 mod 2N: only such a modulus has N slots (CG_EINVAL otherwise).  Synchronises the device,
+ * as does cg_req_destroy. */
 int cg_req_create(cg_req **out, cg_ctx *ctx, const cg_params *prm);
 int cg_req_destroy(cg_req *req);
 

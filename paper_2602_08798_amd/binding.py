@@ -25,7 +25,7 @@ _SYMBOLS = [
     "cg_mul_relin_static", "cg_static_scratch_bytes",
     "cg_rotate_hoisted", "cg_prefill_qk_hoisted", "cg_prefill_av_hoisted", "cg_cpvm_hoisted",
     "cg_rotate_sum_hoisted", "cg_round_galois", "cg_decode_scores_hoisted", "cg_decode_context_hoisted",
-    "cg_decode_step_hoisted", "cg_mul_sum",
+    "cg_decode_step_hoisted", "cg_mul_sum", "cg_check_params",
 ]
 # libcryptogen_requests.so
 _REQUEST_SYMBOLS = [
@@ -116,6 +116,7 @@ class Library:
         d.cg_create.argtypes = [C.POINTER(vp), C.POINTER(_Params)]
         d.cg_destroy.argtypes = [vp]
         d.cg_get_sizes.argtypes = [vp, C.POINTER(_Sizes)]
+        d.cg_check_params.argtypes = [vp, C.POINTER(_Params)]
         d.cg_workspace_bytes.argtypes = [vp, u32]
         d.cg_workspace_bytes.restype = C.c_size_t
         d.cg_strerror.argtypes = [i32]

@@ -499,6 +499,19 @@ extern "C" int cg_get_sizes(const cg_ctx *c, cg_sizes *o)
     return CG_OK;
 }
 
+extern "C" int cg_check_params(const cg_ctx *c, const cg_params *prm)
+{
+    CG_REQUIRE(c && prm && prm->q);
+    CG_REQUIRE(prm->log2n == (uint32_t)c->logn && prm->k == (uint32_t)c->k && prm->nsp == (uint32_t)c->nsp && prm->alpha == (uint32_t)c->alpha &&
+               prm->t == c->t);
+    for (int i = 0; i < c->k; i++) CG_REQUIRE(prm->q[i] == c->pr[i]);
+    for (int i = 0; prm->p && i < c->nsp; i++) CG_REQUIRE(prm->p[i] == c->pr[c->k + i]);
+    int dev;
+    CG_HIP(hipGetDevice(&dev));
+    CG_REQUIRE(dev == c->device);
+    return CG_OK;
+}
+
 extern "C" size_t cg_workspace_bytes(const cg_ctx *c, uint32_t batch)
 {
     if (!c) return 0;

@@ -230,10 +230,8 @@ CG_API int cg_req_create(cg_req **out, cg_ctx *ctx, const cg_params *prm)
     const uint64_t N = 1ull << prm->log2n;
     CG_REQUIRE(prm->t < (1u << 20) && prm->t % (2 * N) == 1 && small_prime(prm->t));
     for (uint32_t i = 0; i < prm->k; i++) CG_REQUIRE(prm->q[i] % (2 * N) == 1 && prm->q[i] > (1ull << 40) && prm->q[i] < (1ull << 50));
-    // the context has these sizes
-    cg_sizes z;
-    CG_TRY(cg_get_sizes(ctx, &z));
-    CG_REQUIRE(z.ct2_bytes == 2 * prm->k * N * 8 && z.ksk_raw_bytes == (size_t)(prm->k / prm->alpha) * 2 * (prm->k + prm->nsp) * N * 8);
+    // the tables made here are used with the context's
+    CG_TRY(cg_check_params(ctx, prm));
     cg_req *c = new (std::nothrow) cg_req();
     if (!c) return CG_ENOMEM;
     c->ctx = ctx;
