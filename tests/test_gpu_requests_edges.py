@@ -81,3 +81,48 @@ def test_appends_of_the_largest_products(name):
                     v = np.array([int(p) * int(half[i]) * int(s) % m for p, s in zip(points[r, c, i], sign)], dtype=np.uint64)
                     want = (bfv.ntt_inverse(v, m).astype(object) + (m - 1)) % m
                     assert np.array_equal(got[r, 0, 0, c, i].astype(object), want), (what, kind, c, i)
+
+
+@pytest.mark.parametrize("log2n,tops", [(12, (50, 41)), (13, (41, 41, 50)), (14, (41, 50))])
+def test_primes_of_different_sizes(log2n, tops):
+    """Ciphertext primes just above 2^40 beside ones just below 2^50: bounds that are stated for the largest hold for the smallest too."""
+    import torch
+    import paper_2602_08798_amd as P
+    from oracle import Oracle, attention
+    from oracle.client import SlotCodec, galois_rot
+    from tests.bruteforce import ntt_primes
+    from workloads import Stream, pseudo_ciphertexts, pseudo_switch_key
+    from workloads.params import ParamSet
+    n = 1 << log2n
+    pool = {41: ntt_primes(1 << 41, 2 * n, 4), 50: ntt_primes(1 << 50, 2 * n, 4)}
+    q, p = tuple(pool[top].pop(0) for top in tops), (pool[50].pop(0),)
+    prm = ParamSet("x", log2n, q=q, p=p)
+    ctx, orc, codec, k = P.Context(prm), Oracle(prm), SlotCodec(prm), len(q)
+    rq, dev, d2 = P.Requests(ctx), P.to_device, 64
+    rng = np.random.default_rng(log2n)
+    say(f"N = {n}: primes of {tops} bits")
+    v = rng.integers(-128, 128, (9, n))
+    v[0], v[1] = (prm.t - 1) // 2, -((prm.t - 1) // 2)
+    polys = np.stack([codec.encode(x) for x in v])
+    assert torch.equal(rq.slots_prepare(_ints(v)), ctx.plain_prepare(dev(polys)))
+    x = pseudo_ciphertexts(Stream(5, 1), q, n, 2)
+    x[0] = np.array(q, dtype=np.uint64)[:, None] - 1
+    gens = attention.block_generators(n, d2)
+    rounds = [g for r in attention.round_galois(n, gens, 3) for g in r]
+    raw = {g: pseudo_switch_key(Stream(6, g), list(q) + list(p), n, prm.dnum) for g in dict.fromkeys([galois_rot(n, 1)] + rounds)}
+    keys = {g: ctx.ksk_prepare(dev(r)) for g, r in raw.items()}
+    diags, low = ctx.plain_prepare(dev(polys[:2])), ctx.plain_prepare(dev(polys[2:4]))
+    got = P.to_host(rq.cpvm_requests(dev(x), diags, 2, 1, 2, d2, [keys[galois_rot(n, 1)]], [keys[g] for g in rounds], adapters=low,
+                                     pick=_ints([0, -1], torch.int32), block_round_bits=3))
+    for r in range(2):
+        want = attention.cpvm_with_adapter(orc, x[r], list(polys[:2]), None if r else list(polys[2:4]), raw, d2, w=3)
+        assert np.array_equal(got[r, 0], want), r
+    table, edges = _ints([[100], [-100]]), _ints([0, 7], torch.int32)
+    out = P.to_host(rq.score_bias(dev(x), 2, 1, 1, d2, _ints([9, n // d2 - 1], torch.int32), table, edges))
+    for r, pos in enumerate((9, n // d2 - 1)):
+        bias = codec.encode(attention.score_bias_values(n, d2, 0, pos, [[100], [-100]], [0, 7], 0))
+        assert np.array_equal(out[r], orc.add_plain(x[r], bias)), r
+    cache = dev(x)
+    rq.kv_append_requests(cache, 1, 2, 1, _ints([1, 0], torch.int32), dev(x[::-1].copy()), diags, n // 2)
+    got = P.to_host(cache)
+    assert np.array_equal(got[0], orc.add(x[0], orc.mul_plain(x[1], polys[1]))) and np.array_equal(got[1], orc.mul_plain(x[0], polys[0]))
