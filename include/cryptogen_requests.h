@@ -11,9 +11,9 @@
  *
  * Conventions are those of cryptogen.h (device buffers of the caller, 16-byte aligned; canonical residues;
  * errors; outputs must not overlap inputs unless stated), with these additions:
- *   integers    int64 plaintext values are any representatives modulo t in (-2^31, 2^31); slot s of a
- *               plaintext is its value at zeta^e, e = 3^i for s = i < N/2 and -3^i for s = N/2 + i (mod 2N),
- *               zeta the smallest primitive 2N-th root of unity modulo t.
+ *   integers    int64 plaintext values are any representatives modulo t; slot s of a plaintext is its value at
+ *               zeta^e, e = 3^i for s = i < N/2 and -3^i for s = N/2 + i (mod 2N), zeta the smallest
+ *               primitive 2N-th root of unity modulo t.
  *   int32       arrays of one entry per request or bucket need only 4-byte alignment.
  *   device      every call needs the handle's device to be the current one (CG_EINVAL otherwise; for create it
  *               is the context's, and destroy waits for the current one).

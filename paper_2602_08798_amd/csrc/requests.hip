@@ -168,7 +168,7 @@ int create(cg_req *c, const cg_params *prm)
     }
     c->T = Tables{reinterpret_cast<DevConst *>(to[0]), reinterpret_cast<double *>(to[1]), reinterpret_cast<double *>(to[2]),
                   reinterpret_cast<uint16_t *>(to[3]), reinterpret_cast<float *>(to[4]), reinterpret_cast<uint16_t *>(to[5]),
-                  H.ninv[k], logn, k};
+                  H.ninv[k], centred((1ull << 32) % prm->t, prm->t), logn, k};
     return hipDeviceSynchronize() == hipSuccess ? CG_OK : CG_EHIP;
 }
 

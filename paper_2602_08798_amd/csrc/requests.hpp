@@ -14,8 +14,15 @@ struct Tables {
     const float *zeta;         // zeta^e mod t, centred, e < 2N
     const uint16_t *pow3;      // 3^i mod 2N, i < N/2
     double ninv_t;             // N^-1 mod t, centred
+    double two32_t;            // 2^32 mod t, centred
     int logn, k;
 };
+// v modulo t, exact and below 2^51 (a product of 2^31 and a residue below 2^19, and 2^32): red() leaves at most (1/2 + 2^-15) t of it, which is below
+// 2^19 for every t with slots (the largest is 1032193).  Any int64 costs no more than its low half did: 128 plaintexts 20.7 us, before 20.9.
+__device__ __forceinline__ double of_int64(int64_t v, double two32_t)
+{
+    return __builtin_fma((double)(int)(v >> 32), two32_t, (double)(uint32_t)v);
+}
 
 // workgroups of 1024 threads with rows of 8192 in at most 64 registers a thread: two of them on a compute unit
 template <int LOGN, int E> constexpr int two_waves() { return LOGN == 13 && E == 8 ? 8 : min_waves<LOGN, E>(); }
@@ -115,7 +122,7 @@ __device__ __forceinline__ void small_inv_row(double *lds, double *out, int tid,
 struct LdSlots {
     const int64_t *v;
     int logn;
-    __device__ __forceinline__ double value(int b, int slot) const { return (double)(int)at32(v + ((size_t)b << logn), slot); }
+    __device__ __forceinline__ double value(int b, int slot, double two32_t) const { return of_int64(at32(v + ((size_t)b << logn), slot), two32_t); }
 };
 // slot `slot` of diagonal c of unit u, b = u n_diag + c: M[f][col], f the feature that the token's copy c shows there, col = slot mod d2
 struct Diagonal {
@@ -130,15 +137,15 @@ struct Diagonal {
 };
 struct LdMatrix : Diagonal {        // int64 [units][d1][d2]
     const int64_t *m;
-    __device__ __forceinline__ double value(int b, int slot) const
+    __device__ __forceinline__ double value(int b, int slot, double two32_t) const
     {
         const int f = feature(b, slot);
-        return f < d1 ? (double)(int)m[(((size_t)(b >> log_diag) * d1 + f) << log_d2) + col(slot)] : 0.0;
+        return f < d1 ? of_int64(m[(((size_t)(b >> log_diag) * d1 + f) << log_d2) + col(slot)], two32_t) : 0.0;
     }
 };
 struct LdSkewed : Diagonal {        // float [units][tile][d2], row (f - col) mod tile: the d2 slots of a block lie in one row
     const float *m;
-    __device__ __forceinline__ double value(int b, int slot) const
+    __device__ __forceinline__ double value(int b, int slot, double) const
     {
         const int f = feature(b, slot), row = (f - col(slot)) & ((1 << log_tile) - 1);
         return f < d1 ? (double)m[(((((size_t)(b >> log_diag)) << log_tile) + row) << log_d2) + col(slot)] : 0.0;
@@ -157,7 +164,7 @@ encode_kernel(LD ld, void *__restrict__ out, Tables T, int whole, int split)
     const ModD mt = T.C->mod[k];
     double v[E], w[E];
 #pragma unroll
-    for (int it = 0; it < E; it++) v[it] = ld.value(b, tid + it * TH);
+    for (int it = 0; it < E; it++) v[it] = ld.value(b, tid + it * TH, T.two32_t);
 #pragma unroll
     for (int it = 0; it < E; it++) lds[pad((int)at_lane(T.place + it * TH, tid))] = red(v[it], mt);
     lds_barrier();
@@ -214,13 +221,13 @@ low_rank_kernel(const int64_t *__restrict__ w, const int64_t *__restrict__ a, co
     cg_double4v acc[4] = {};
     // (W's words come in beside the products)
     const int64_t *wu = w + (((size_t)u * d1) << log_d2);
-    int base[4][4];
+    double base[4][4];
 #pragma unroll
     for (int c = 0; c < 4; c++)
 #pragma unroll
         for (int e = 0; e < 4; e++) {
             const int f = f0 + 16 * wave + 4 * e + q, col = c0 + 16 * c + i;
-            base[c][e] = w && f < d1 && col < d2 ? (int)at32(wu, (f << log_d2) + col) : 0;
+            base[c][e] = w && f < d1 && col < d2 ? of_int64(at32(wu, (f << log_d2) + col), T.two32_t) : 0.0;
         }
     for (int j0 = 0; j0 < rank; j0 += LR_RANK) {
         int64_t x[4], y[4];
@@ -233,8 +240,8 @@ low_rank_kernel(const int64_t *__restrict__ w, const int64_t *__restrict__ a, co
         if (j0) __syncthreads();
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-            as[tid >> 2][4 * (tid & 3) + e] = red((double)(int)x[e], mt);
-            bs[tid >> 4][4 * (tid & 15) + e] = red((double)(int)y[e], mt);
+            as[tid >> 2][4 * (tid & 3) + e] = red(of_int64(x[e], T.two32_t), mt);
+            bs[tid >> 4][4 * (tid & 15) + e] = red(of_int64(y[e], T.two32_t), mt);
         }
         __syncthreads();
 #pragma unroll
@@ -248,7 +255,7 @@ low_rank_kernel(const int64_t *__restrict__ w, const int64_t *__restrict__ a, co
 #pragma unroll
     for (int c = 0; c < 4; c++)
 #pragma unroll
-        for (int e = 0; e < 4; e++) done[16 * wave + 4 * e + q][16 * c + i] = (float)red(red(acc[c][e], mt) + (double)base[c][e], mt);
+        for (int e = 0; e < 4; e++) done[16 * wave + 4 * e + q][16 * c + i] = (float)red(red(acc[c][e], mt) + base[c][e], mt);
     __syncthreads();
     // feature - column = dd - 63 within the tile: a row of the layout to a wave at a time
     float *mine = out + (((size_t)u * tile) << log_d2);
@@ -437,7 +444,7 @@ struct BiasArgs {
     const int32_t *edges;
     int n_buckets, heads, n_cts, log_d2;
     // bias of distance `dist`, and head h
-    __device__ __forceinline__ double bias(int dist, int h, const ModD mt) const
+    __device__ __forceinline__ double bias(int dist, int h, const ModD mt, double two32_t) const
     {
         if (dist < 0) return 0.0;
         int lo = 0;                      // edges at or below the distance
@@ -450,7 +457,7 @@ struct BiasArgs {
                 else hi = mid;
             }
         }
-        return lo ? red((double)(int)table[(size_t)(lo - 1) * heads + h], mt) : 0.0;
+        return lo ? red(of_int64(table[(size_t)(lo - 1) * heads + h], two32_t), mt) : 0.0;
     }
 };
 constexpr int BIAS_THREADS = 256;
@@ -486,7 +493,7 @@ bias_kernel(BiasArgs A, Tables T)
         }
         int at = (int)(T.pow3[b << ld2] >> (ld2 + 2));      // (3^(d2 b) - 1) / (4 d2)
         if (row) at = (np - at) & (np - 1);
-        ab[row * np + (int)(__brev((unsigned)at) >> (32 - log_np))] = (float)A.bias(dist, h, mt);
+        ab[row * np + (int)(__brev((unsigned)at) >> (32 - log_np))] = (float)A.bias(dist, h, mt, T.two32_t);
     }
     __syncthreads();
     for (int s = 0; s < log_np; s++) {

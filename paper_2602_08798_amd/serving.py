@@ -104,7 +104,7 @@ class Requests:
         return batch, self._at(slots, _I64, 0, "slots")
 
     def slots_encode(self, slots, out=None):
-        """int64 slot values [..., N], any representatives in (-2^31, 2^31) -> polynomials with coefficients in [0, t)."""
+        """int64 slot values [..., N], any representatives modulo t -> polynomials with coefficients in [0, t)."""
         batch, at = self._batch(slots)
         out = torch.empty_like(slots) if out is None else out
         self._call("cg_slots_encode", at, self._at(out, _I64, batch * self.n, "out"), batch)

@@ -126,3 +126,37 @@ def test_primes_of_different_sizes(log2n, tops):
     rq.kv_append_requests(cache, 1, 2, 1, _ints([1, 0], torch.int32), dev(x[::-1].copy()), diags, n // 2)
     got = P.to_host(cache)
     assert np.array_equal(got[0], orc.add(x[0], orc.mul_plain(x[1], polys[1]))) and np.array_equal(got[1], orc.mul_plain(x[0], polys[0]))
+
+
+@pytest.mark.parametrize("name", ["C1", "C2", "C5"])
+def test_any_int64_is_a_representative(name):
+    """Slots, matrices, factors and tables whose values fill 64 bits give what their residues give."""
+    import torch
+    env = _env(name)
+    n, t, rq = env.n, env.prm.t, env.rq
+    rng = np.random.default_rng(17)
+    ends = np.array([2 ** 63 - 1, -(2 ** 63), 2 ** 32 - 1, 2 ** 32, -(2 ** 32), -(2 ** 31), 2 ** 31, -(2 ** 31) - 1, -1, 0], dtype=np.int64)
+
+    def wide(*shape):
+        v = rng.integers(-(2 ** 63), 2 ** 63 - 1, shape, dtype=np.int64, endpoint=True)
+        v.reshape(-1)[:len(ends)] = ends
+        return v, v % t
+
+    say(f"{name}: slots")
+    v, r = wide(9, n)
+    assert torch.equal(rq.slots_encode(_ints(v)), rq.slots_encode(_ints(r)))
+    assert torch.equal(rq.slots_prepare(_ints(v)), rq.slots_prepare(_ints(r)))
+    units, d1, d2 = 2, 100, 64
+    w, a, b = wide(units, d1, d2), wide(1, d1, 5), wide(units, 5, d2)
+    for given in ((True, False), (False, True), (True, True)):       # W as it is given, A B, W beside A B
+        say(f"{name}: matrices {given}")
+        got, want = (rq.cpvm_prepare(units, d1, d2, w=_ints(w[i]) if given[0] else None, a=_ints(a[i]) if given[1] else None,
+                                     b=_ints(b[i]) if given[1] else None, a_group=units) for i in range(2))
+        assert torch.equal(got, want), given
+    many = 1 + 256 // rq.cpvm_diagonals(d1, d2)                      # so many that they are laid out by diagonals first
+    w = wide(many, d1, d2)
+    assert torch.equal(*(rq.cpvm_prepare(many, d1, d2, w=_ints(x)) for x in w))
+    say(f"{name}: tables")
+    table, edges = wide(5, 2), _ints([0, 1, 2, 3, 4], torch.int32)
+    s = env.dev(env.cts(2, 2))
+    assert torch.equal(*(rq.score_bias(s, 1, 2, 1, d2, _ints([4], torch.int32), _ints(x), edges) for x in table))
