@@ -173,16 +173,15 @@ int create(cg_req *c, const cg_params *prm)
 }
 
 // Prepared plaintexts of a last round that leaves compute units free are shared by several workgroups, which repeat the interpolation and
-// divide the primes (at N = 4096, where several workgroups fit a unit, only where no round is full).  us, a workgroup each / shared, N = 8192: 1
-// 22.5 / 12.9, 85 24.7 / 16.3, 128 25.5 / 21.6, 288 47.7 / 38.5, 341 48.5 / 41.1; N = 4096: 1 10.2 / 7.8, 128 11.6 / 9.3, 300 17.9 / 17.9; N = 16384: 1
-// 72.9 / 24.1, 86 76.5 / 48.6, 300 157 / 120.  From a full round on rows of 8192 take 512 threads: 288 38.6 / 35.0, 512 52.2 / 48.5, 1000 103 / 95.7
-// (below, 128 23.5 / 25.4).
+// divide the primes.  us, a workgroup each / shared.  N = 8192, three primes: 1 21.3 / 12.0, 85 23.2 / 15.2, 128 23.9 / 20.8, 288 41.4 / 32.6, 341
+// 41.9 / 34.6, 600 61.0 / 58.0.  N = 4096, two primes: 1 9.5 / 7.2, 128 10.7 / 8.6, 300 16.7 / 14.5, 600 24.8 / 22.6, 1100 38.2 / 35.7; six: 300
+// 34.8 / 27.1.  N = 16384, six: 1 72.2 / 22.9, 86 75.1 / 49.0, 300 153 / 120; two: 300 69.9 / 61.4.  (Where more than half the units are busy nothing is shared.)
 template <bool PREPARED, class LD>
 int encode(const cg_req *c, void *s, LD ld, void *out, uint32_t batch)
 {
     const int cu = c->n_cu, rest = (int)batch % cu;
     int whole = (int)batch, split = 1;
-    if (PREPARED && rest && ((int)batch < cu || c->logn > 12)) {
+    if (PREPARED && rest) {
         const int most = std::min(c->k, cu / rest), each = (c->k + most - 1) / most;      // primes a workgroup
         split = (c->k + each - 1) / each;
         whole -= rest;
@@ -298,7 +297,9 @@ CG_API uint32_t cg_cpvm_diagonals(const cg_req *c, uint32_t d1, uint32_t d2)
 }
 
 // Whether matrices are laid out by their diagonals before these are encoded.  Along a diagonal of a matrix as it is given every lane reads
-// another row: us, 768 x 64 at N = 8192, straight / laid out first: 1 matrix 14.4 / 21.0, 12 26.7 / 31.7, 36 52.0 / 43.5, 72 97.4 / 65.0.
+// another row: us, 768 x 64 at N = 8192, straight / laid out first: 1 matrix 14.1 / 19.6, 12 25.9 / 29.7, 24 35.1 / 37.4, 32 (a plaintext for every unit) 40.3
+// / 38.7, 36 51.3 / 44.3, 72 95.2 / 69.9.  At N = 4096 16 (a plaintext for every unit) 18.6 / 23.4, 20 24.0 / 26.7, 36 39.7 / 34.8, 72 68.1 / 53.0; at
+// N = 16384 72 130.5 / 131.0, 144 256 / 250.  Matrices of few rows stay in the caches: 300 of 100 x 64 at N = 4096 27.4 / 34.8.
 static bool skewed_first(const cg_req *c, uint64_t plaintexts, uint32_t rank) { return rank || plaintexts > (uint32_t)c->n_cu; }
 
 CG_API size_t cg_cpvm_prepare_workspace_bytes(const cg_req *c, uint32_t units, uint32_t d1, uint32_t d2, uint32_t rank)
