@@ -448,7 +448,10 @@ struct BiasArgs {
     {
         if (dist < 0) return 0.0;
         int lo = 0;                      // edges at or below the distance
-        if (n_buckets <= 64) {           // all of them as scalar loads at once, where a search waits for each of its steps
+        // A few as scalar loads at once, where a search waits for each of its steps; a prompt's workgroups, with more of them, hide more of the
+        // loop.  us, loop / search, N = 8192: 384 ciphertexts of scores 8 buckets 28.2 / 28.9, 32 28.7 / 29.2, 64 29.6 / 29.3, 128 34.8 / 29.6 (one 16 5.9 / 5.8,
+        // 64 7.6 / 6.0; 384 of N = 4096 and 256 tokens 32 14.3 / 13.0, 64 16.3 / 13.2); 1536 of a prompt 32 106 / 110, 64 108 / 112, 128 112 / 112.
+        if (n_buckets <= (pos ? 32 : 64)) {
             for (int i = 0; i < n_buckets; i++) lo += edges[i] <= dist;
         } else {
             for (int hi = n_buckets; lo < hi;) {

@@ -160,3 +160,37 @@ def test_any_int64_is_a_representative(name):
     table, edges = wide(5, 2), _ints([0, 1, 2, 3, 4], torch.int32)
     s = env.dev(env.cts(2, 2))
     assert torch.equal(*(rq.score_bias(s, 1, 2, 1, d2, _ints([4], torch.int32), _ints(x), edges) for x in table))
+
+
+@pytest.mark.parametrize("name,batch", [("C1", 300), ("C1", 513), ("C1", 700), ("C2", 257), ("C5", 270)])
+def test_plaintexts_of_a_last_round(name, batch):
+    """The last round's plaintexts, shared by several workgroups where it leaves room, are those of a call of their own."""
+    import torch
+    env = _env(name)
+    say(f"slots_prepare {name}: {batch}")
+    v = _ints(np.random.default_rng(batch).integers(-(2 ** 31), 2 ** 31, (batch, env.n)))
+    got, polys = env.rq.slots_prepare(v), env.rq.slots_encode(v)
+    assert torch.equal(got, env.ctx.plain_prepare(polys))
+    assert torch.equal(got.view(batch, -1)[-1], env.rq.slots_prepare(v[-1:]))
+
+
+@pytest.mark.parametrize("buckets", [32, 33, 64, 65])
+def test_bucket_edges_are_found_by_either_way(buckets):
+    """Around the numbers of buckets from which they are searched: every distance, edges that repeat and that lie beyond the cache."""
+    import torch
+    from oracle import attention
+    env = _env("C1")
+    d2 = 64
+    blocks = env.n // d2
+    say(f"biases: {buckets} buckets")
+    rng = np.random.default_rng(buckets)
+    edges = np.sort(rng.integers(0, blocks + 20, buckets))
+    table = rng.integers(-128, 128, (buckets, 1))
+    x = env.cts(3, blocks)
+    got = env.host(env.rq.score_bias(env.dev(x[:2]), 2, 1, 1, d2, _ints([blocks - 1, blocks // 2], torch.int32), _ints(table),
+                                     _ints(edges, torch.int32)))
+    for r, pos in enumerate((blocks - 1, blocks // 2)):
+        assert np.array_equal(got[r], env.orc.add_plain(x[r], env.codec.encode(attention.score_bias_values(env.n, d2, 0, pos, table, edges, 0)))), r
+    got = env.host(env.rq.prompt_bias(env.dev(x), 1, 1, d2, _ints(table), _ints(edges, torch.int32)))
+    for u in (0, 1, blocks // 2, blocks - 1):
+        assert np.array_equal(got[u], env.orc.add_plain(x[u], env.codec.encode(attention.prompt_bias_values(env.n, d2, u, table, edges, 0)))), u
