@@ -144,7 +144,8 @@ class Requests:
                       block_round_bits=0):
         """y[r][u] = x_r (W_u + the adapter pick[r] asks for), as Context.cpvm_hoisted computes it for one request: adapters
         prepared [n_adapters][units][n_diag] without W, pick int32 [requests] on the GPU (anything else than 0 .. n_adapters - 1:
-        none)."""
+        none).  In rounds of three bits (block_round_bits=3) it takes about
+        half the time it takes generator by generator (0), with more keys."""
         ctx, R, U, D, d2 = self.ctx, _count(requests), _count(units), _count(n_diag), _count(d2)
         out = ctx.empty_ct(R, U) if out is None else out
         ctx._need_keys(list(gk_copies) + list(gk_block))
