@@ -114,7 +114,7 @@ __device__ __forceinline__ void small_inv_row(double *lds, double *out, int tid,
 // Slot values -> polynomial modulo t -> prepared plaintext.  The interpolation is an inverse transform modulo t of the
 // values in the order of the transform's outputs; its results are centred in registers and go through one forward
 // transform per ciphertext prime without leaving the workgroup.  Values are read in the order of the slots, which their
-// sources hold side by side, and put in their places in LDS (read in the order of the places 300 plaintexts took 52.4 us, now 47.9).
+// sources hold side by side, and put in their places in LDS (read in the order of the places 300 plaintexts took 52.4 us where they took 47.9).
 // Bound by vector issue: 1000 plaintexts of N = 8192 and three primes take 86 us, 21.5 ns a row transform, their 262 MB at the rate of a
 // copy would take 49; in 75 registers with one workgroup to a unit 102, with the interpolation by the passes for 50-bit primes 93.6.  One plaintext
 // takes 12.0 us with its primes on workgroups of their own, one after the other 21.3; its polynomial alone 7.3 (1000 of them 29.3).
